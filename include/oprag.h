@@ -14,6 +14,11 @@
  * oprag_search_hybrid_weighted (the paper's weighted score fusion), plus the dense-first
  * serving schedule of Sections 4.1 and 5.5, oprag_search_hybrid_dense_first.
  *
+ * Beside the paper's calls: rows held in few bits and their inner products
+ * (oprag_mx_quantize, oprag_mx_values, oprag_mx_scores, oprag_mx_scores_grad) and the
+ * distillation loss that brings such scores towards ranked lists (oprag_distill_loss,
+ * oprag_distill_grad, oprag_distill_step).
+ *
  * Conventions for every function:
  *  - Return value: OPRAG_OK (0) or a negative oprag_status; the reason is available from
  *    oprag_last_error() (thread-local string).  Nothing throws across the ABI.
@@ -290,6 +295,98 @@ oprag_status oprag_time_next_dense_kernel(void *start_event, void *stop_event);
  */
 #define OPRAG_PROBE_MAX_BLOCKS 4096
 oprag_status oprag_probe_read(const void *src_dev, size_t bytes, int32_t blocks, uint32_t *sink_dev, void *stream);
+
+/*
+ * Rows in the microscaled format: a row of dim elements is nb = ceil(dim / 32) blocks of 32, the
+ * last one padded with zeros.  Block j of a row is one scale byte c and 32 element codes; element
+ * i of the block stands for 2^(c - 127) times the value of code i.  c = 255 makes every element
+ * of the block NaN.  Codes are of one width:
+ *   bits 4 (e2m1): sign and 0, 0.5, 1, 1.5, 2, 3, 4, 6;
+ *   bits 6 (e2m3): sign and i / 8 below 1, then (1 + i / 8) 2^e for e = 0, 1, 2 (up to 7.5);
+ * packed from the lowest bit of a block's first byte on: 16 or 24 bytes a block.
+ *   codes_dev  [* x nb x 4 bits] bytes, scales_dev [* x nb] bytes: both caller-owned, row-major.
+ * The rows meant are [first_row, first_row + rows) of the arrays.  1 <= dim <= OPRAG_MAX_DIM;
+ * first_row + rows <= 2^31 - 2.
+ */
+typedef struct oprag_mx_rows {
+  void *codes_dev;
+  uint8_t *scales_dev;
+  int64_t first_row;
+  int64_t rows;
+  int32_t dim;
+  int32_t bits; /* 4 or 6 */
+} oprag_mx_rows;
+
+/*
+ * Quantises out->rows rows of x (x_dtype; row i at x_dev + i x_ld elements, x_ld >= dim) into
+ * `out`.  A block's scale is c = max(floor(log2 amax) - 2 + 127, 0) with amax its largest
+ * magnitude (0 for a block of zeros); an element becomes the nearest code to x / 2^(c - 127) (a tie
+ * to the even code), at most the largest.  A block with an infinity or a NaN gets c = 255 and
+ * zero codes.  rows = 0 is a no-op.  Asynchronous on `stream`.
+ */
+oprag_status oprag_mx_quantize(const void *x_dev, int32_t x_dtype, int64_t x_ld, const oprag_mx_rows *out,
+                               void *stream);
+
+/* The values that `rows` stand for, [rows x dim] in out_dtype (row i at out_dev + i out_ld
+ * elements, out_ld >= dim; rounded to nearest even where the type cannot hold them). */
+oprag_status oprag_mx_values(const oprag_mx_rows *rows, void *out_dev, int32_t out_dtype, int64_t out_ld,
+                             void *stream);
+
+/*
+ * Inner products S[q, i] of every row of `q` with every row of `rows` (equal dim; the bits may
+ * differ), summed in fp32 and rounded once to out_dtype: S[q, i] at out_dev + q out_ld + i
+ * elements, out_ld >= rows->rows.  No rows on either side is a no-op.  Asynchronous on `stream`.
+ */
+oprag_status oprag_mx_scores(const oprag_mx_rows *q, const oprag_mx_rows *rows, void *out_dev, int32_t out_dtype,
+                             int64_t out_ld, void *stream);
+
+/*
+ * The gradient of those products, straight through the quantisation: given G = dL/dS,
+ *   transposed = 0: out = G X,   G [m x x->rows]  (the queries' gradient; X the rows),
+ *   transposed = 1: out = G^T X, G [x->rows x m]  (the rows' gradient; X the queries),
+ * out [m x dim] fp32 (row i at out_dev + i out_ld, out_ld >= dim).  G is grad_dtype with row
+ * stride grad_ld elements.  Every product of a grad element and a value is exact or in fp32, sums
+ * are fp32 in a fixed order.  x->rows = 0 makes out zero.  workspace_dev must hold
+ * oprag_mx_scores_grad_bytes(m, x) bytes.  Asynchronous on `stream`.
+ */
+oprag_status oprag_mx_scores_grad_bytes(int64_t m, const oprag_mx_rows *x, size_t *bytes);
+oprag_status oprag_mx_scores_grad(const void *grad_dev, int32_t grad_dtype, int64_t grad_ld, int32_t transposed,
+                                  int64_t m, const oprag_mx_rows *x, float *out_dev, int64_t out_ld,
+                                  void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * Distillation of scores towards ranked lists.  Query q's student is the softmax over all n rows,
+ * z_i = logits[q, i] / temperature, lse = log sum_i exp z_i.  Its teacher is the softmax p of
+ * t_scores / teacher_temperature over the list's entries: those with an id in [0, n) and a score
+ * above -inf (so the -1 / -inf padding of the searches' lists is left out).  Then
+ *   loss[q]    = sum over entries of p (log p - z_id + lse)         (Kullback-Leibler divergence),
+ *   grad[q, i] = weight[q] / temperature * (exp(z_i - lse) - sum of p over the entries with id i).
+ * A list without entries has loss 0 and gradient 0.  A logit of -inf (a masked row) has probability
+ * 0; an entry with p > 0 on such a row makes the loss +inf.  With an entry in the list, a NaN or
+ * +inf among the logits, or a +inf teacher score, makes the query's loss and gradient NaN.
+ *   logits_dev [nq x n] in dtype (row stride ld elements);  ids_dev [nq x k] int64, t_scores_dev
+ *   [nq x k] fp32;  loss_dev, lse_dev, weight_dev [nq] fp32;  grad_dev [nq x n] in dtype (row
+ *   stride grad_ld; it may be logits_dev itself with grad_ld = ld).
+ * Arithmetic is fp32 or more.  1 <= k <= OPRAG_MAX_K; temperatures are normal numbers > 0.
+ *   oprag_distill_loss: loss and lse;
+ *   oprag_distill_grad: grad, given oprag_distill_loss's lse;
+ *   oprag_distill_step: loss and grad at once, where the weight is known ahead of the loss.
+ * workspace_dev must hold oprag_distill_bytes(nq, n) bytes (loss and step).  Asynchronous on
+ * `stream`.
+ */
+oprag_status oprag_distill_bytes(int64_t nq, int64_t n, size_t *bytes);
+oprag_status oprag_distill_loss(const void *logits_dev, int32_t dtype, int64_t ld, int64_t nq, int64_t n,
+                                const int64_t *ids_dev, const float *t_scores_dev, int32_t k, float temperature,
+                                float teacher_temperature, float *loss_dev, float *lse_dev, void *workspace_dev,
+                                size_t workspace_bytes, void *stream);
+oprag_status oprag_distill_grad(const void *logits_dev, int32_t dtype, int64_t ld, int64_t nq, int64_t n,
+                                const int64_t *ids_dev, const float *t_scores_dev, int32_t k, float temperature,
+                                float teacher_temperature, const float *lse_dev, const float *weight_dev,
+                                void *grad_dev, int64_t grad_ld, void *stream);
+oprag_status oprag_distill_step(const void *logits_dev, int32_t dtype, int64_t ld, int64_t nq, int64_t n,
+                                const int64_t *ids_dev, const float *t_scores_dev, int32_t k, float temperature,
+                                float teacher_temperature, const float *weight_dev, float *loss_dev, void *grad_dev,
+                                int64_t grad_ld, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -19,6 +19,8 @@ values, with no blocking, fusion or pruning:
 * ``accept`` - the tie-aware acceptance rules the GPU results are held to.
 * ``dense_first``, ``weighted``, ``embed_tail`` - the dense-first hybrid schedule, the
   paper's weighted score fusion and the mean-pool + L2 tail of the embedding step.
+* ``mx``, ``distill`` - rows in few bits, their products and the products' gradient; the
+  distillation loss of such scores and its gradient.
 
 Where the paper is silent, each module's docstring states the reading it takes.
 """

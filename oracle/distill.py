@@ -1,0 +1,59 @@
+"""Distillation of scores towards ranked lists.  Test infrastructure only.
+
+Per query: z = logits / tau over all n rows, lse = log sum exp z; the teacher p is the softmax of
+t / t_tau over the list's entries, those with an id in [0, n) and a score above -inf (an id may
+come twice: its entries' probabilities then add up in the gradient).
+
+* loss = sum over entries of p (log p - (z_id - lse)); 0 for a list without entries, +inf if an entry
+  with p > 0 meets a logit of -inf;
+* d(weight loss) / d logits_i = weight / tau (exp(z_i - lse) - sum of p over entries with id i); 0 for a list
+  without entries; a logit of -inf has probability 0, also where every logit is -inf.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+
+
+def teacher(ids, t, n: int, t_tau: float):
+    """[(id, p, log p)] of one list's entries."""
+    at = [(int(i), float(s) / t_tau) for i, s in zip(ids, t) if 0 <= i < n and s > -math.inf]
+    if not at:
+        return []
+    top = max(u for _, u in at)
+    if math.isinf(top):
+        return [(i, math.nan, math.nan) for i, _ in at]
+    mass = sum(math.exp(u - top) for _, u in at)
+    return [(i, math.exp(u - top) / mass, u - top - math.log(mass)) for i, u in at]
+
+
+def distill(logits, ids, t, tau: float, t_tau: float, weight=None):
+    """(loss [nq], lse [nq], grad [nq x n]) in fp64."""
+    s = np.asarray(logits, dtype=np.float64)
+    nq, n = s.shape
+    loss, lse, grad = np.zeros(nq), np.full(nq, -np.inf), np.zeros((nq, n))
+    for q in range(nq):
+        z = s[q] / tau
+        prob = np.zeros(n)
+        if n and (np.isnan(z).any() or (z == np.inf).any()):
+            lse[q] = np.nan
+            prob[:] = np.nan
+        elif n and (z > -np.inf).any():
+            top = z.max()
+            e = np.exp(z - top)
+            lse[q] = top + math.log(e.sum())
+            prob = e / e.sum()
+        entries = teacher(ids[q], t[q], n, t_tau)
+        if not entries:
+            continue
+        g = prob.copy()
+        for i, p, logp in entries:
+            g[i] -= p
+            if math.isnan(p) or math.isnan(lse[q]):
+                loss[q] = math.nan
+            elif p > 0:
+                loss[q] += math.inf if z[i] == -np.inf else p * (logp - (z[i] - lse[q]))
+        w = 1.0 if weight is None else float(weight[q])
+        grad[q] = w / tau * g if not any(math.isnan(p) for _, p, _ in entries) else math.nan
+    return loss, lse, grad

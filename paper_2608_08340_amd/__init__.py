@@ -11,6 +11,13 @@ the library raises ``OpragError`` if ``liboprag.so`` is missing (build it with
     scores, ids = idx.search_dense(queries, k=5)       # Op_retrieve, exact top-k
     idx.attach_sparse(term_indptr, post_chunk, post_tf, doc_len)
     fused, ids = idx.search_hybrid(queries, qterm_indptr, qterms)
+
+Rows in few bits, their inner products, and the loss that fits queries to ranked lists:
+
+    rows = mx_quantize(idx.rows(), bits=4)             # 4.25 bits per element
+    logits = mx_scores(mx_quantize(queries, bits=6), rows)
+    loss, dlogits = distill_step(logits, ids, scores, weight, temperature=0.05)
+    dqueries = mx_scores_grad(dlogits, rows)
 """
 from __future__ import annotations
 
@@ -20,8 +27,9 @@ import threading
 
 import torch
 
-__all__ = ["Index", "OpragError", "rrf_fuse", "library", "LIB_PATH", "OP_DENSE", "OP_SPARSE", "OP_HYBRID",
-           "OP_DENSE_FIRST", "OP_WEIGHTED"]
+__all__ = ["Index", "MxRows", "OpragError", "distill_grad", "distill_loss", "distill_step", "mx_quantize", "mx_scores",
+           "mx_scores_grad", "mx_values", "rrf_fuse", "library", "LIB_PATH", "OP_DENSE", "OP_SPARSE",
+           "OP_HYBRID", "OP_DENSE_FIRST", "OP_WEIGHTED"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liboprag.so")
 OP_DENSE, OP_SPARSE, OP_HYBRID, OP_DENSE_FIRST, OP_WEIGHTED = 0, 1, 2, 3, 4
@@ -40,8 +48,14 @@ class _Desc(ctypes.Structure):
                 ("device", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class _MxDesc(ctypes.Structure):
+    _fields_ = [("codes_dev", ctypes.c_void_p), ("scales_dev", ctypes.c_void_p), ("first_row", ctypes.c_int64),
+                ("rows", ctypes.c_int64), ("dim", ctypes.c_int32), ("bits", ctypes.c_int32)]
+
+
 _P = ctypes.c_void_p
 _I32, _I64, _SZ, _F = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
+_MX = ctypes.POINTER(_MxDesc)
 _SIGS = {
     "oprag_abi_version": ([], _I32),
     "oprag_last_error": ([], ctypes.c_char_p),
@@ -62,6 +76,15 @@ _SIGS = {
                                      _I32),
     "oprag_time_next_dense_kernel": ([_P, _P], _I32),
     "oprag_probe_read": ([_P, _SZ, _I32, _P, _P], _I32),
+    "oprag_mx_quantize": ([_P, _I32, _I64, _MX, _P], _I32),
+    "oprag_mx_values": ([_MX, _P, _I32, _I64, _P], _I32),
+    "oprag_mx_scores": ([_MX, _MX, _P, _I32, _I64, _P], _I32),
+    "oprag_mx_scores_grad_bytes": ([_I64, _MX, ctypes.POINTER(_SZ)], _I32),
+    "oprag_mx_scores_grad": ([_P, _I32, _I64, _I32, _I64, _MX, _P, _I64, _P, _SZ, _P], _I32),
+    "oprag_distill_bytes": ([_I64, _I64, ctypes.POINTER(_SZ)], _I32),
+    "oprag_distill_loss": ([_P, _I32, _I64, _I64, _I64, _P, _P, _I32, _F, _F, _P, _P, _P, _SZ, _P], _I32),
+    "oprag_distill_grad": ([_P, _I32, _I64, _I64, _I64, _P, _P, _I32, _F, _F, _P, _P, _P, _I64, _P], _I32),
+    "oprag_distill_step": ([_P, _I32, _I64, _I64, _I64, _P, _P, _I32, _F, _F, _P, _P, _P, _I64, _P, _SZ, _P], _I32),
 }
 _lib = None
 _lock = threading.Lock()
@@ -141,6 +164,10 @@ class Index:
 
     def __len__(self) -> int:
         return self.n_rows
+
+    def rows(self) -> torch.Tensor:
+        """The stored rows [n_rows x dim], a view of the slab."""
+        return self.slab[:self.n_rows]
 
     # ------------------------------------------------------------------ upsert
     def upsert(self, rows: torch.Tensor) -> int:
@@ -329,3 +356,216 @@ def time_next_dense_kernel(start: torch.cuda.Event | None, stop: torch.cuda.Even
     a = ctypes.c_void_p(start.cuda_event) if start is not None else None
     b = ctypes.c_void_p(stop.cuda_event) if stop is not None else None
     _check(library().oprag_time_next_dense_kernel(a, b))
+
+
+# ---------------------------------------------------------------------- rows in few bits
+def _run(device: torch.device, name: str, *args) -> None:
+    """Calls the library on `device`'s current stream (the last argument of every such call)."""
+    fn = getattr(library(), name)
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, _stream(device)))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(device)))
+
+
+def _on_gpu(device: torch.device) -> torch.device:
+    if device.type != "cuda":
+        raise OpragError(-1, f"tensors must be on a GPU, not on {device}")
+    return device
+
+
+def _matrix(t: torch.Tensor, device, shape, name: str, dtype=None) -> int:
+    """The row stride of a row-major matrix, checked."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.device != device:
+        raise OpragError(-1, f"{name} must be a matrix on {device}")
+    if t.dtype not in _DTYPE or (dtype is not None and t.dtype != dtype):
+        raise OpragError(-1, f"unsupported {name} dtype {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise OpragError(-1, f"{name} must be {list(shape)}, not {list(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise OpragError(-1, f"{name} must have contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else max(1, t.shape[1])
+
+
+class MxRows:
+    """Rows in the microscaled format: per block of 32 elements one scale byte and 32 codes of 4 bits
+    (e2m1) or 6 bits (e2m3); include/oprag.h states the values.
+
+    ``codes`` uint8 [n, ceil(dim / 32), 16 or 24] and ``scales`` uint8 [n, ceil(dim / 32)] are plain
+    tensors that a caller may keep, copy or allocate ahead (``MxRows.empty``); ``part`` is a view
+    of some of the rows, to append to or to score a shard of.
+    """
+
+    __slots__ = ("codes", "scales", "dim", "bits", "first", "n")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, dim: int, first: int = 0, n: int | None = None):
+        dim = int(dim)
+        nb = (dim + 31) // 32
+        if codes.dim() != 3 or codes.shape[2] not in (16, 24) or codes.shape[1] != nb:
+            raise OpragError(-1, f"codes must be [n, {nb}, 16 or 24] for dim {dim}, not {list(codes.shape)}")
+        if tuple(scales.shape) != tuple(codes.shape[:2]):
+            raise OpragError(-1, f"scales must be {list(codes.shape[:2])}, not {list(scales.shape)}")
+        _dev_tensor(codes, torch.uint8, codes.device, "codes")
+        _dev_tensor(scales, torch.uint8, codes.device, "scales")
+        n = codes.shape[0] - first if n is None else n
+        if first < 0 or n < 0 or first + n > codes.shape[0]:
+            raise OpragError(-1, f"rows [{first}, {first + n}) outside [0, {codes.shape[0]})")
+        self.codes, self.scales, self.dim, self.bits = codes, scales, dim, codes.shape[2] // 4
+        self.first, self.n = first, n
+
+    @classmethod
+    def empty(cls, n: int, dim: int, bits: int = 4, device: int | torch.device = 0) -> "MxRows":
+        if bits not in (4, 6):
+            raise OpragError(-1, f"bits = {bits} is not 4 or 6")
+        dev = torch.device("cuda", device) if isinstance(device, int) else device
+        nb = (int(dim) + 31) // 32
+        return cls(torch.empty((n, nb, 4 * bits), dtype=torch.uint8, device=dev),
+                   torch.empty((n, nb), dtype=torch.uint8, device=dev), dim)
+
+    def part(self, first: int, n: int) -> "MxRows":
+        """Rows [first, first + n), sharing this object's memory."""
+        if first < 0 or n < 0 or first + n > self.n:
+            raise OpragError(-1, f"rows [{first}, {first + n}) outside [0, {self.n})")
+        return MxRows(self.codes, self.scales, self.dim, self.first + first, n)
+
+    def __len__(self) -> int:
+        return self.n
+
+    @property
+    def device(self) -> torch.device:
+        return self.codes.device
+
+    def _desc(self) -> _MxDesc:
+        return _MxDesc(self.codes.data_ptr(), self.scales.data_ptr(), self.first, self.n, self.dim, self.bits)
+
+
+def _mx(rows, device, name: str) -> MxRows:
+    if not isinstance(rows, MxRows) or rows.device != device:
+        raise OpragError(-1, f"{name} must be MxRows on {device}")
+    return rows
+
+
+def mx_quantize(x: torch.Tensor, bits: int = 4, out: MxRows | None = None) -> MxRows:
+    """Quantises rows [n x dim] (fp32, bf16 or fp16; rows may be strided), into `out` if given."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise OpragError(-1, "x must be a matrix")
+    _on_gpu(x.device)
+    ld = _matrix(x, x.device, x.shape, "x")
+    if out is None:
+        out = MxRows.empty(x.shape[0], x.shape[1], bits, x.device)
+    elif len(_mx(out, x.device, "out")) != x.shape[0] or out.dim != x.shape[1] or out.bits != bits:
+        raise OpragError(-1, f"out must hold {x.shape[0]} rows of {x.shape[1]} elements in {bits} bits")
+    _run(x.device, "oprag_mx_quantize", _ptr(x), _DTYPE[x.dtype], ld, out._desc())
+    return out
+
+
+def mx_values(rows: MxRows, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values that quantised rows stand for, [n x dim]."""
+    dev = _on_gpu(_mx(rows, getattr(rows, "device", None), "rows").device)
+    if out is None:
+        out = torch.empty((len(rows), rows.dim), dtype=dtype, device=dev)
+    ld = _matrix(out, dev, (len(rows), rows.dim), "out", dtype)
+    _run(dev, "oprag_mx_values", rows._desc(), _ptr(out), _DTYPE[dtype], ld)
+    return out
+
+
+def mx_scores(q: MxRows, rows: MxRows, dtype: torch.dtype = torch.float32,
+              out: torch.Tensor | None = None) -> torch.Tensor:
+    """Inner products [len(q) x len(rows)], summed in fp32, in `dtype`."""
+    dev = _on_gpu(_mx(q, getattr(q, "device", None), "q").device)
+    _mx(rows, dev, "rows")
+    if out is None:
+        out = torch.empty((len(q), len(rows)), dtype=dtype, device=dev)
+    ld = _matrix(out, dev, (len(q), len(rows)), "out", dtype)
+    _run(dev, "oprag_mx_scores", q._desc(), rows._desc(), _ptr(out), _DTYPE[dtype], ld)
+    return out
+
+
+def mx_scores_grad(grad: torch.Tensor, x: MxRows, transposed: bool = False,
+                   out: torch.Tensor | None = None) -> torch.Tensor:
+    """The gradient of ``mx_scores``, straight through the quantisation, fp32: to the queries grad @
+    values(x) with x the rows, or, transposed, to the rows grad.T @ values(x) with x the queries."""
+    dev = _on_gpu(_mx(x, getattr(x, "device", None), "x").device)
+    if not isinstance(grad, torch.Tensor) or grad.dim() != 2:
+        raise OpragError(-1, "grad must be a matrix")
+    m = grad.shape[1] if transposed else grad.shape[0]
+    ld = _matrix(grad, dev, (len(x), m) if transposed else (m, len(x)), "grad")
+    if out is None:
+        out = torch.empty((m, x.dim), dtype=torch.float32, device=dev)
+    out_ld = _matrix(out, dev, (m, x.dim), "out", torch.float32)
+    desc, need = x._desc(), ctypes.c_size_t()
+    _check(library().oprag_mx_scores_grad_bytes(m, desc, ctypes.byref(need)))
+    ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+    _run(dev, "oprag_mx_scores_grad", _ptr(grad), _DTYPE[grad.dtype], ld, int(transposed), m, desc, _ptr(out), out_ld,
+                                          _ptr(ws), need.value)
+    return out
+
+
+# ---------------------------------------------------------------------- distillation
+def _distill_args(logits, teacher_ids, teacher_scores, temperature, teacher_temperature):
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+        raise OpragError(-1, "logits must be a matrix")
+    dev = _on_gpu(logits.device)
+    ld = _matrix(logits, dev, logits.shape, "logits")
+    _dev_tensor(teacher_ids, torch.int64, dev, "teacher_ids")
+    _dev_tensor(teacher_scores, torch.float32, dev, "teacher_scores")
+    nq, n = logits.shape
+    if teacher_ids.dim() != 2 or teacher_ids.shape[0] != nq or teacher_scores.shape != teacher_ids.shape:
+        raise OpragError(-1, f"teacher_ids and teacher_scores must both be [{nq} x k]")
+    return dev, (_ptr(logits), _DTYPE[logits.dtype], ld, nq, n, _ptr(teacher_ids), _ptr(teacher_scores),
+                 teacher_ids.shape[1], temperature, teacher_temperature)
+
+
+def _distill_ws(dev, nq: int, n: int):
+    need = ctypes.c_size_t()
+    _check(library().oprag_distill_bytes(nq, n, ctypes.byref(need)))
+    return (torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None), need.value
+
+
+def _vector(t, n: int, dev, name: str) -> torch.Tensor:
+    if _dev_tensor(t, torch.float32, dev, name).shape != (n,):
+        raise OpragError(-1, f"{name} must have {n} entries")
+    return t
+
+
+def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_scores: torch.Tensor, temperature: float = 1.0,
+                 teacher_temperature: float = 1.0):
+    """Kullback-Leibler divergence, per query, of the student (softmax of logits / temperature over all
+    rows) from the teacher (softmax of the ranked list's scores / teacher_temperature; padding is
+    left out). Returns (loss, lse), fp32 [nq]; the gradient needs lse."""
+    dev, a = _distill_args(logits, teacher_ids, teacher_scores, temperature, teacher_temperature)
+    nq, n = logits.shape
+    loss = torch.empty(nq, dtype=torch.float32, device=dev)
+    lse = torch.empty(nq, dtype=torch.float32, device=dev)
+    ws, size = _distill_ws(dev, nq, n)
+    _run(dev, "oprag_distill_loss", *a, _ptr(loss), _ptr(lse), _ptr(ws), size)
+    return loss, lse
+
+
+def distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_scores: torch.Tensor, lse: torch.Tensor,
+                 weight: torch.Tensor, temperature: float = 1.0, teacher_temperature: float = 1.0,
+                 out: torch.Tensor | None = None) -> torch.Tensor:
+    """The gradient of sum(weight * loss) to the logits, in their dtype; `out` may be the logits."""
+    dev, a = _distill_args(logits, teacher_ids, teacher_scores, temperature, teacher_temperature)
+    nq, n = logits.shape
+    _vector(lse, nq, dev, "lse")
+    _vector(weight, nq, dev, "weight")
+    out = torch.empty((nq, n), dtype=logits.dtype, device=dev) if out is None else out
+    out_ld = _matrix(out, dev, (nq, n), "out", logits.dtype)
+    _run(dev, "oprag_distill_grad", *a, _ptr(lse), _ptr(weight), _ptr(out), out_ld)
+    return out
+
+
+def distill_step(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_scores: torch.Tensor, weight: torch.Tensor,
+                 temperature: float = 1.0, teacher_temperature: float = 1.0, out: torch.Tensor | None = None):
+    """Loss [nq] and the gradient of sum(weight * loss) to the logits in one call; `out` may be the logits."""
+    dev, a = _distill_args(logits, teacher_ids, teacher_scores, temperature, teacher_temperature)
+    nq, n = logits.shape
+    _vector(weight, nq, dev, "weight")
+    loss = torch.empty(nq, dtype=torch.float32, device=dev)
+    out = torch.empty((nq, n), dtype=logits.dtype, device=dev) if out is None else out
+    out_ld = _matrix(out, dev, (nq, n), "out", logits.dtype)
+    ws, size = _distill_ws(dev, nq, n)
+    _run(dev, "oprag_distill_step", *a, _ptr(weight), _ptr(loss), _ptr(out), out_ld, _ptr(ws), size)
+    return loss, out

@@ -18,7 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liboprag.so")
 SOURCES = ["api.cpp", "dense.hip", "dense_tile_bf16.hip", "dense_tile_f16.hip", "dense_tile_f32.hip", "bm25.hip",
-           "fuse_upsert.hip"]
+           "fuse_upsert.hip", "mx_quant.hip", "mx_scores.hip", "mx_grad.hip", "distill.hip"]
 ARCH = "gfx950"
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

@@ -208,6 +208,78 @@ oprag_status scratch_of(int device, void** out) {
   return OPRAG_OK;
 }
 
+// ---------------------------------------------------------------- rows in few bits, distillation
+constexpr int64_t kMaxRows = (int64_t)0x7ffffffe;
+
+oprag_status check_count(int64_t v, const char* name) {
+  if (v < 0 || v > kMaxRows) return fail(OPRAG_E_INVALID, "%s = %lld outside [0, 2^31 - 2]", name, (long long)v);
+  return OPRAG_OK;
+}
+
+// A caller's row-major matrix of rows x cols elements, `ld` apart.  Its pointer is looked at only if it has elements.
+oprag_status check_matrix(const void* p, int32_t dtype, int64_t ld, int64_t rows, int64_t cols, const char* name) {
+  if (!valid_dtype(dtype)) return fail(OPRAG_E_INVALID, "%s: dtype %d is not an oprag_dtype", name, dtype);
+  if (rows == 0 || cols == 0) return OPRAG_OK;
+  if (ld < cols || ld > (int64_t)1 << 31)
+    return fail(OPRAG_E_INVALID, "%s: row stride %lld outside [%lld, 2^31]", name, (long long)ld, (long long)cols);
+  if (!p) return fail(OPRAG_E_INVALID, "%s is NULL", name);
+  if (!aligned16(p)) return fail(OPRAG_E_INVALID, "%s is not 16-byte aligned", name);
+  return OPRAG_OK;
+}
+
+oprag_status check_mx(const oprag_mx_rows* r, const char* name, oprag::MxRows* out) {
+  if (!r) return fail(OPRAG_E_INVALID, "%s is NULL", name);
+  if (r->bits != 4 && r->bits != 6) return fail(OPRAG_E_INVALID, "%s: bits = %d is not 4 or 6", name, r->bits);
+  if (r->dim < 1 || r->dim > OPRAG_MAX_DIM)
+    return fail(OPRAG_E_INVALID, "%s: dim %d outside [1, %d]", name, r->dim, OPRAG_MAX_DIM);
+  if (r->rows < 0 || r->first_row < 0 || r->rows > kMaxRows || r->first_row > kMaxRows - r->rows)
+    return fail(OPRAG_E_INVALID, "%s: rows [%lld, + %lld) outside [0, 2^31 - 2]", name, (long long)r->first_row,
+                (long long)r->rows);
+  out->rows = r->rows;
+  out->dim = r->dim;
+  out->bits = r->bits;
+  out->nb = (r->dim + 31) / 32;
+  if (r->rows == 0) return OPRAG_OK;
+  if (!r->codes_dev || !r->scales_dev) return fail(OPRAG_E_INVALID, "%s: codes_dev or scales_dev is NULL", name);
+  if (!aligned16(r->codes_dev) || !aligned16(r->scales_dev))
+    return fail(OPRAG_E_INVALID, "%s: codes_dev or scales_dev is not 16-byte aligned", name);
+  out->codes = static_cast<unsigned char*>(r->codes_dev) + (size_t)r->first_row * out->nb * (4 * r->bits);
+  out->scales = r->scales_dev + (size_t)r->first_row * out->nb;
+  return OPRAG_OK;
+}
+
+oprag_status check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (need && (!ws || !aligned16(ws) || bytes < need))
+    return fail(OPRAG_E_INVALID, "workspace missing, misaligned or too small (%zu < %zu bytes)", bytes, need);
+  return OPRAG_OK;
+}
+
+oprag_status check_distill(const void* logits, int32_t dtype, int64_t ld, int64_t nq, int64_t n, const int64_t* ids,
+                           const float* t, int32_t k, float tau, float t_tau, oprag::DistillArgs* a) {
+  if (oprag_status st = check_count(nq, "nq")) return st;
+  if (oprag_status st = check_count(n, "n")) return st;
+  if (oprag_status st = check_k(k, "k")) return st;
+  if (!(std::isnormal(tau) && tau > 0.f)) return fail(OPRAG_E_INVALID, "temperature must be a normal number > 0");
+  if (!(std::isnormal(t_tau) && t_tau > 0.f))
+    return fail(OPRAG_E_INVALID, "teacher_temperature must be a normal number > 0");
+  if (oprag_status st = check_matrix(logits, dtype, ld, n ? nq : 0, n, "logits")) return st;
+  if (nq) {
+    if (oprag_status st = check_buf(ids, "ids_dev")) return st;
+    if (oprag_status st = check_buf(t, "t_scores_dev")) return st;
+  }
+  a->logits = logits;
+  a->dtype = dtype;
+  a->ld = ld;
+  a->nq = nq;
+  a->n = n;
+  a->ids = reinterpret_cast<const long long*>(ids);
+  a->t = t;
+  a->k = k;
+  a->tau = tau;
+  a->t_tau = t_tau;
+  return OPRAG_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -744,6 +816,141 @@ oprag_status oprag_search_hybrid_weighted(const oprag_index* idx, const void* q_
                                     mm_d, p.n_chunks, mm_l, pl, (double)w_dense, (double)w_lex, k, cbuf, ccnt,
                                     scores_dev, reinterpret_cast<long long*>(ids_dev), s);
   if (e != hipSuccess) return hip_fail(e, "weighted fusion launch");
+  return ok();
+}
+
+oprag_status oprag_mx_quantize(const void* x_dev, int32_t x_dtype, int64_t x_ld, const oprag_mx_rows* out,
+                               void* stream) {
+  oprag::MxRows r;
+  if (oprag_status st = check_mx(out, "out", &r)) return st;
+  if (oprag_status st = check_matrix(x_dev, x_dtype, x_ld, r.rows, r.dim, "x")) return st;
+  if (r.rows == 0) return ok();
+  const hipError_t e = oprag::launch_mx_quantize(x_dev, x_dtype, x_ld, r, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "quantisation launch");
+  return ok();
+}
+
+oprag_status oprag_mx_values(const oprag_mx_rows* rows, void* out_dev, int32_t out_dtype, int64_t out_ld,
+                             void* stream) {
+  oprag::MxRows r;
+  if (oprag_status st = check_mx(rows, "rows", &r)) return st;
+  if (oprag_status st = check_matrix(out_dev, out_dtype, out_ld, r.rows, r.dim, "out")) return st;
+  if (r.rows == 0) return ok();
+  const hipError_t e = oprag::launch_mx_values(r, out_dev, out_dtype, out_ld, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "values launch");
+  return ok();
+}
+
+oprag_status oprag_mx_scores(const oprag_mx_rows* q, const oprag_mx_rows* rows, void* out_dev, int32_t out_dtype,
+                             int64_t out_ld, void* stream) {
+  oprag::MxRows a, b;
+  if (oprag_status st = check_mx(q, "q", &a)) return st;
+  if (oprag_status st = check_mx(rows, "rows", &b)) return st;
+  if (a.dim != b.dim) return fail(OPRAG_E_INVALID, "q has dim %d, rows have dim %d", a.dim, b.dim);
+  if (oprag_status st = check_matrix(out_dev, out_dtype, out_ld, b.rows ? a.rows : 0, b.rows, "out")) return st;
+  if (a.rows == 0 || b.rows == 0) return ok();
+  const hipError_t e = oprag::launch_mx_scores(a, b, out_dev, out_dtype, out_ld, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "scores launch");
+  return ok();
+}
+
+oprag_status oprag_mx_scores_grad_bytes(int64_t m, const oprag_mx_rows* x, size_t* bytes) {
+  if (!bytes) return fail(OPRAG_E_INVALID, "bytes is NULL");
+  oprag::MxRows r;
+  if (oprag_status st = check_mx(x, "x", &r)) return st;
+  if (oprag_status st = check_count(m, "m")) return st;
+  *bytes = oprag::mx_grad_workspace_bytes(m, r);
+  return ok();
+}
+
+oprag_status oprag_mx_scores_grad(const void* grad_dev, int32_t grad_dtype, int64_t grad_ld, int32_t transposed,
+                                  int64_t m, const oprag_mx_rows* x, float* out_dev, int64_t out_ld,
+                                  void* workspace_dev, size_t workspace_bytes, void* stream) {
+  oprag::MxRows r;
+  if (oprag_status st = check_mx(x, "x", &r)) return st;
+  if (oprag_status st = check_count(m, "m")) return st;
+  if (transposed != 0 && transposed != 1) return fail(OPRAG_E_INVALID, "transposed = %d is not 0 or 1", transposed);
+  const int64_t g_rows = transposed ? r.rows : m, g_cols = transposed ? m : r.rows;
+  if (oprag_status st = check_matrix(grad_dev, grad_dtype, grad_ld, g_cols ? g_rows : 0, g_cols, "grad")) return st;
+  if (oprag_status st = check_matrix(out_dev, OPRAG_F32, out_ld, m, r.dim, "out")) return st;
+  if (m == 0) return ok();
+  const size_t need = oprag::mx_grad_workspace_bytes(m, r);
+  if (oprag_status st = check_workspace(workspace_dev, workspace_bytes, need)) return st;
+  const hipError_t e = oprag::launch_mx_grad(grad_dev, grad_dtype, grad_ld, transposed != 0, m, r, out_dev, out_ld,
+                                             workspace_dev, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "scores gradient launch");
+  return ok();
+}
+
+oprag_status oprag_distill_bytes(int64_t nq, int64_t n, size_t* bytes) {
+  if (!bytes) return fail(OPRAG_E_INVALID, "bytes is NULL");
+  if (oprag_status st = check_count(nq, "nq")) return st;
+  if (oprag_status st = check_count(n, "n")) return st;
+  *bytes = oprag::distill_workspace_bytes(nq, n);
+  return ok();
+}
+
+oprag_status oprag_distill_loss(const void* logits_dev, int32_t dtype, int64_t ld, int64_t nq, int64_t n,
+                                const int64_t* ids_dev, const float* t_scores_dev, int32_t k, float temperature,
+                                float teacher_temperature, float* loss_dev, float* lse_dev, void* workspace_dev,
+                                size_t workspace_bytes, void* stream) {
+  oprag::DistillArgs a;
+  if (oprag_status st = check_distill(logits_dev, dtype, ld, nq, n, ids_dev, t_scores_dev, k, temperature,
+                                      teacher_temperature, &a))
+    return st;
+  if (nq == 0) return ok();
+  if (oprag_status st = check_buf(loss_dev, "loss_dev")) return st;
+  if (oprag_status st = check_buf(lse_dev, "lse_dev")) return st;
+  const size_t need = oprag::distill_workspace_bytes(nq, n);
+  if (oprag_status st = check_workspace(workspace_dev, workspace_bytes, need)) return st;
+  a.loss = loss_dev;
+  a.lse = lse_dev;
+  const hipError_t e = oprag::launch_distill(a, workspace_dev, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "distillation loss launch");
+  return ok();
+}
+
+oprag_status oprag_distill_grad(const void* logits_dev, int32_t dtype, int64_t ld, int64_t nq, int64_t n,
+                                const int64_t* ids_dev, const float* t_scores_dev, int32_t k, float temperature,
+                                float teacher_temperature, const float* lse_dev, const float* weight_dev,
+                                void* grad_dev, int64_t grad_ld, void* stream) {
+  oprag::DistillArgs a;
+  if (oprag_status st = check_distill(logits_dev, dtype, ld, nq, n, ids_dev, t_scores_dev, k, temperature,
+                                      teacher_temperature, &a))
+    return st;
+  if (oprag_status st = check_matrix(grad_dev, dtype, grad_ld, n ? nq : 0, n, "grad")) return st;
+  if (nq == 0 || n == 0) return ok();
+  if (oprag_status st = check_buf(lse_dev, "lse_dev")) return st;
+  if (oprag_status st = check_buf(weight_dev, "weight_dev")) return st;
+  a.lse_in = lse_dev;
+  a.weight = weight_dev;
+  a.grad = grad_dev;
+  a.grad_ld = grad_ld;
+  const hipError_t e = oprag::launch_distill(a, nullptr, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "distillation gradient launch");
+  return ok();
+}
+
+oprag_status oprag_distill_step(const void* logits_dev, int32_t dtype, int64_t ld, int64_t nq, int64_t n,
+                                const int64_t* ids_dev, const float* t_scores_dev, int32_t k, float temperature,
+                                float teacher_temperature, const float* weight_dev, float* loss_dev, void* grad_dev,
+                                int64_t grad_ld, void* workspace_dev, size_t workspace_bytes, void* stream) {
+  oprag::DistillArgs a;
+  if (oprag_status st = check_distill(logits_dev, dtype, ld, nq, n, ids_dev, t_scores_dev, k, temperature,
+                                      teacher_temperature, &a))
+    return st;
+  if (oprag_status st = check_matrix(grad_dev, dtype, grad_ld, n ? nq : 0, n, "grad")) return st;
+  if (nq == 0) return ok();
+  if (oprag_status st = check_buf(loss_dev, "loss_dev")) return st;
+  if (oprag_status st = check_buf(weight_dev, "weight_dev")) return st;
+  const size_t need = oprag::distill_workspace_bytes(nq, n);
+  if (oprag_status st = check_workspace(workspace_dev, workspace_bytes, need)) return st;
+  a.loss = loss_dev;
+  a.weight = weight_dev;
+  a.grad = grad_dev;
+  a.grad_ld = grad_ld;
+  const hipError_t e = oprag::launch_distill(a, workspace_dev, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "distillation step launch");
   return ok();
 }
 

@@ -228,4 +228,39 @@ hipError_t launch_probe_read(const void* src, long long bytes, unsigned int* sin
 hipError_t launch_upsert(void* slab, int slab_dtype, int d, long long first_row, const void* rows,
                          int rows_dtype, long long m, hipStream_t s);
 
+// ---------------------------------------------------------------- rows in few bits
+// Rows in the microscaled format (oprag_mx_rows; the pointers are at the first row meant).
+struct MxRows {
+  unsigned char* codes = nullptr;  // [rows x nb x 4 bits] bytes
+  unsigned char* scales = nullptr; // [rows x nb]
+  long long rows = 0;
+  int dim = 0, bits = 0, nb = 0;   // nb = ceil(dim / 32)
+};
+hipError_t launch_mx_quantize(const void* x, int dtype, long long ld, const MxRows& out, hipStream_t s);
+hipError_t launch_mx_values(const MxRows& rows, void* out, int dtype, long long ld, hipStream_t s);
+hipError_t launch_mx_scores(const MxRows& q, const MxRows& rows, void* out, int dtype, long long ld, hipStream_t s);
+size_t mx_grad_workspace_bytes(long long m, const MxRows& x);
+hipError_t launch_mx_grad(const void* grad, int dtype, long long ld, bool transposed, long long m, const MxRows& x,
+                          float* out, long long out_ld, void* ws, hipStream_t s);
+
+// ---------------------------------------------------------------- distillation
+struct DistillArgs {
+  const void* logits = nullptr;  // [nq x n], row stride ld
+  int dtype = 0;
+  long long ld = 0, nq = 0, n = 0;
+  const long long* ids = nullptr;  // [nq x k]
+  const float* t = nullptr;        // [nq x k]
+  int k = 0;
+  float tau = 1.f, t_tau = 1.f;
+  const float* weight = nullptr;   // grad, step: [nq]
+  const float* lse_in = nullptr;   // grad: [nq]
+  float* loss = nullptr;           // loss, step: [nq]
+  float* lse = nullptr;            // loss: [nq]
+  void* grad = nullptr;            // grad, step: [nq x n], row stride grad_ld
+  long long grad_ld = 0;
+};
+size_t distill_workspace_bytes(long long nq, long long n);
+// loss and lse (no grad pointer), grad from lse_in (no loss pointer), or loss and grad.
+hipError_t launch_distill(const DistillArgs& a, void* ws, hipStream_t s);
+
 }  // namespace oprag
