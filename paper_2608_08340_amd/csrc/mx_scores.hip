@@ -1,14 +1,20 @@
 // Inner products of rows in the microscaled format (oprag_mx_scores).
 //
 // S[q, i] = sum over blocks b of 2^(cq + ci - 254) sum_j q[b, j] x[b, j].  One scaled matrix instruction takes 16 rows
-// and 16 queries over 128 elements (four blocks), in 4 or 6 bits, and applies both scale bytes of
-// every block itself; its sums are fp32.
+// and 16 queries over 128 elements (four blocks: a step), in 4 or 6 bits, and applies both scale
+// bytes of every block itself; its sums are fp32.  A lane l holds block l / 16 of row l % 16.
 //
-// A workgroup of four waves keeps a block of QT x 16 queries in LDS and passes over a run of row
-// tiles.  A wave owns RT x 16 rows of a tile: it loads their codes and scales straight into
-// registers (no other wave needs them), sixteen blocks ahead of the product that uses them, and
-// reads the queries' fragments from LDS, where they lie in the order of the lanes.  The rows that a
-// lane loads are permuted so that its sums are of RT x 4 consecutive rows, which it stores as one piece.
+// A workgroup keeps a block of QT x 16 queries in LDS and passes over a run of row tiles.  A wave
+// owns RT x 16 rows of a tile and loads them straight into registers (no other wave needs them),
+// a set of four steps ahead of the products.  Four neighbouring lanes load 64 (96) contiguous bytes of one
+// row, then of the next, and exchange them: lane by lane as the instruction wants its
+// operands, every load would touch 64 cache lines.  (Measured so: 2 TB/s of rows at best.)
+// Which blocks of a set make a step is free, as long as both sides agree: lane group a = l / 16
+// has blocks 4 a .. 4 a + 3, one per step, so its four scale bytes are one dword.  Of a last set of
+// s < 4 steps it has blocks s a .. s a + s - 1.
+//
+// The sums pass by the caches (nontemporal): kept there, they push out the rows that the other
+// query blocks of the chunk are about to read (1,024 x 262,144 fp32: 430 us, 270 without them).
 #include <algorithm>
 
 #include "mfma.h"
@@ -26,223 +32,300 @@ struct ScoresArgs {
   void* out;
   long long ld;
   int dtype;
-  int n_qblocks, n_chunks;  // chunk c takes row tiles [c tiles / n_chunks, (c + 1) tiles / n_chunks)
-  long long tiles;
-};
-
-// One lane's share of a block: 16 or 24 bytes.
-template <int BITS>
-struct Codes {
-  static constexpr int kWords = BITS;
-  unsigned w[BITS];
-  __device__ __forceinline__ void load(const unsigned char* p) {
-    const uint4 a = *reinterpret_cast<const uint4*>(__builtin_assume_aligned(p, BITS == 4 ? 16 : 8));
-    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
-    if constexpr (BITS == 6) {
-      const uint2 b = *reinterpret_cast<const uint2*>(p + 16);
-      w[4] = b.x, w[5] = b.y;
-    }
-  }
-  __device__ __forceinline__ i32x8 operand() const {
-    i32x8 v = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
-    if constexpr (BITS == 6) v[4] = (int)w[4], v[5] = (int)w[5];
-    return v;
-  }
+  int n_qblocks, n_chunks;
+  int least, spare;  // row tiles of a chunk; the first `spare` chunks have one more
 };
 
 template <int RB, int QB, int STEP>
-__device__ __forceinline__ f32x4 mfma_mx(const Codes<RB>& a, unsigned sa, const Codes<QB>& b, unsigned sb, f32x4 c) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.operand(), b.operand(), c, RB == 4 ? 4 : 2, QB == 4 ? 4 : 2,
-                                                          0, (int)sa, STEP, (int)sb);
+__device__ __forceinline__ f32x4 mfma_mx(const unsigned (&a)[RB], unsigned sa, const unsigned (&b)[QB], unsigned sb, f32x4 c) {
+  i32x8 x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+  if constexpr (RB == 6) x[4] = (int)a[4], x[5] = (int)a[5];
+  if constexpr (QB == 6) y[4] = (int)b[4], y[5] = (int)b[5];
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, RB == 4 ? 4 : 2, QB == 4 ? 4 : 2, STEP, (int)sa, STEP, (int)sb);
 }
 
-// Four steps of 128 elements of a wave's rows.
-template <int RB, int RT>
-struct RowSet {
-  Codes<RB> c[RT][4];
-  unsigned s[RT][4];
-};
-
-template <int QT>
-constexpr int lds_steps() {
-  return QT == 8 ? 8 : QT == 4 ? 16 : 32;  // steps of 128 elements of the queries that LDS holds
-}
-
-// N consecutive rows' sums to out[row ..], as many as there are.
-template <typename T, int N>
-__device__ __forceinline__ void store_rows(T* p, const float (&v)[N], long long left) {
-  typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-  if (left >= N) {
-    V o;
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = (T)v[i];
-    *reinterpret_cast<V*>(p) = o;
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < left) p[i] = (T)v[i];
+// A block's 16 or 24 bytes.
+template <int BITS>
+__device__ __forceinline__ void load_block(unsigned (&w)[BITS], const unsigned char* p) {
+  typedef unsigned V4 __attribute__((ext_vector_type(4), aligned(8)));
+  typedef unsigned V2 __attribute__((ext_vector_type(2), aligned(8)));
+  const V4 a = *reinterpret_cast<const V4*>(p);
+  w[0] = a[0], w[1] = a[1], w[2] = a[2], w[3] = a[3];
+  if constexpr (BITS == 6) {
+    const V2 b = *reinterpret_cast<const V2*>(p + 16);
+    w[4] = b[0], w[5] = b[1];
   }
 }
 
-template <int QB, int RB, int RT, int QT>
-__global__ __launch_bounds__(256, 2) void scores_kernel(ScoresArgs p) {
-  constexpr int KC = lds_steps<QT>();
-  // [kc / 4][QT][64] scale bytes of four steps, [kc][QT][64] codes: their first 16 bytes, and the other 8
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  const int kc = min(KC, (p.r.nb + 15) / 16 * 4);
-  unsigned* lds_s = reinterpret_cast<unsigned*>(lds);
-  uint4* lds_lo = reinterpret_cast<uint4*>(lds_s + kc / 4 * QT * 64);
-  uint2* lds_hi = reinterpret_cast<uint2*>(lds_lo + kc * QT * 64);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, g = lane >> 4;
-  const int nb = p.r.nb, steps = (nb + 3) / 4, sets = (steps + 3) / 4;
-  const long long row_bytes = (long long)nb * (4 * RB);
-  const long long items = (long long)p.n_qblocks * p.n_chunks;
-  for (long long item = logical_block(); item < items; item += gridDim.x) {
-    const long long chunk = item / p.n_qblocks, q0 = (item - chunk * p.n_qblocks) * (QT * 16);
-    const long long t0 = chunk * p.tiles / p.n_chunks, t1 = (chunk + 1) * p.tiles / p.n_chunks;
+// The four bytes from p + at on.  Reads none past p + bytes (at least 4): those come back as what they are not.
+__device__ __forceinline__ unsigned load_scales(const unsigned char* p, unsigned at, unsigned bytes) {
+  const unsigned from = min(at, bytes - 4);
+  unsigned v;
+  __builtin_memcpy(&v, p + from, 4);
+  return v >> (8 * min(at - from, 3u));
+}
+// The n bytes (1 to 4) from p on, by the aligned words that hold the first and the last of them.
+__device__ __forceinline__ unsigned load_bytes(const unsigned char* p, int n) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+  const unsigned lo = *reinterpret_cast<const unsigned*>(a & ~uintptr_t(3));
+  const unsigned hi = *reinterpret_cast<const unsigned*>((a + n - 1) & ~uintptr_t(3));
+  return __builtin_amdgcn_alignbyte(hi, lo, (unsigned)a & 3u);
+}
+// The first n of them.
+__device__ __forceinline__ unsigned first_bytes(unsigned v, int n) { return n >= 4 ? v : n <= 0 ? 0u : v & ((1u << 8 * n) - 1); }
 
-    // Queries' steps [first, first + KC) to LDS: zeros, with a scale of one, past the last block and the last query.
+// Four steps of a wave's rows.
+template <int RB, int RT>
+struct RowSet {
+  unsigned w[RT][4][RB];
+  unsigned s[RT];
+};
+
+// Within four neighbouring lanes, lane c's w[i] becomes lane i's w[c].
+template <int RB>
+__device__ __forceinline__ void transpose4(unsigned (&w)[4][RB], bool odd, bool high) {
+#pragma unroll
+  for (int k = 0; k < RB; ++k) {
+    auto swap = [&](unsigned& x, unsigned& y, auto ctrl, bool second) {
+      const unsigned from_y = (unsigned)__builtin_amdgcn_mov_dpp((int)y, ctrl(), 0xf, 0xf, true);
+      const unsigned from_x = (unsigned)__builtin_amdgcn_mov_dpp((int)x, ctrl(), 0xf, 0xf, true);
+      x = second ? from_y : x;
+      y = second ? y : from_x;
+    };
+    constexpr std::integral_constant<int, 0xb1> by1{};  // lanes 1 0 3 2
+    constexpr std::integral_constant<int, 0x4e> by2{};  // lanes 2 3 0 1
+    swap(w[0][k], w[1][k], by1, odd);
+    swap(w[2][k], w[3][k], by1, odd);
+    swap(w[0][k], w[2][k], by2, high);
+    swap(w[1][k], w[3][k], by2, high);
+  }
+}
+
+// Sets (512 elements) of the queries that LDS holds.
+template <int QT>
+constexpr int lds_sets() {
+  return QT == 8 ? 2 : QT == 4 ? 4 : 8;
+}
+
+// N consecutive rows' sums to p; with TAIL, the first `left` of them.
+template <bool TAIL, typename T, int N>
+__device__ __forceinline__ void store_rows(T* p, const float (&v)[N], long long left) {
+  typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+  if constexpr (TAIL) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < left) p[i] = (T)v[i];
+  } else {
+    V o;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = (T)v[i];
+    __builtin_nontemporal_store(o, reinterpret_cast<V*>(p));
+  }
+}
+
+// W waves, each with RT x 16 rows of a tile.  TAIL: the rows fill no tile.  Otherwise the last tile ends with the last
+// row, and computes some rows that the tile before it has too, to the same bits.
+// RES: LDS holds all sets of the queries.
+template <int QB, int RB, int W, int RT, int QT, bool RES, bool TAIL>
+__global__ __launch_bounds__(W * 64, 2) void scores_kernel(ScoresArgs p) {
+  constexpr int KC = lds_sets<QT>(), ROWS = W * RT * 16;
+  // [kc][QT][16 queries][16 blocks] codes, block c of query q at c ^ q: their first 16 bytes, and the
+  // other 8; [kc][QT][64 lanes] scale bytes of a lane's four steps
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const int nb = p.r.nb, sets = (nb + 15) / 16, kc = min(KC, sets);
+  const int end_blocks = nb - 16 * (sets - 1), end_steps = (end_blocks + 3) / 4;  // of the last set
+  uint4* lds_lo = reinterpret_cast<uint4*>(lds);
+  uint2* lds_hi = reinterpret_cast<uint2*>(lds_lo + kc * QT * 256);
+  unsigned* lds_s = reinterpret_cast<unsigned*>(lds + kc * QT * 256 * (4 * QB));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, g = lane >> 4, b4 = (lane >> 2) & 3, c4 = lane & 3;
+  const unsigned row_bytes = (unsigned)nb * (4 * RB);
+  // A lane's stores are of 16 bytes: 4 consecutive rows in fp32, 8 in 16 bits (4 where it has only those).
+  const bool pieces = p.dtype != kDtypeF32 && RT > 1;
+  const int group = pieces ? 8 : 4;  // rows 4 b .. 4 b + 3 of a subtile lie `group` apart in b
+  auto subtile = [&](int t) { return pieces ? 32 * (t >> 1) + 4 * (t & 1) : 16 * t; };
+  const unsigned last_q = (unsigned)p.q.rows - 1, items = (unsigned)p.n_qblocks * (unsigned)p.n_chunks;
+
+  for (unsigned item = (unsigned)logical_block(); item < items; item += gridDim.x) {
+    const unsigned chunk = item / (unsigned)p.n_qblocks, q0 = (item - chunk * (unsigned)p.n_qblocks) * (QT * 16);
+    const long long t0 = (long long)chunk * p.least + min((int)chunk, p.spare), t1 = t0 + p.least + ((int)chunk < p.spare);
+
+    // Sets [first, first + KC) of the queries to LDS.  Past a row's last block both sides take some block's codes
+    // (finite, as any codes are) under the smallest scale: 2^-254 times such products are zero in fp32.
     auto stage = [&](int first) {
       __syncthreads();
-      const int have = min(KC, (steps - first + 3) & ~3);
-      for (int f = wave; f < have * QT; f += 4) {
-        const int st = f / QT, qt = f - st * QT, b = (first + st) * 4 + g;
-        const long long q = q0 + qt * 16 + r16;
-        Codes<QB> c = {};
-        if (b < nb && q < p.q.rows) c.load(p.q.codes + (q * nb + b) * (4 * QB));
-        lds_lo[f * 64 + lane] = make_uint4(c.w[0], c.w[1], c.w[2], c.w[3]);
-        if constexpr (QB == 6) lds_hi[f * 64 + lane] = make_uint2(c.w[4], c.w[5]);
-      }
-      for (int f = wave; f < have / 4 * QT; f += 4) {
-        const int st = f / QT * 4, qt = f % QT;
-        const long long q = q0 + qt * 16 + r16;
-        unsigned v = 0x7f7f7f7fu;
-        if (q < p.q.rows) {
-          v = 0;
+      const int have = min(KC, sets - first);
+      constexpr int kS = (KC * QT + W - 1) / W, kL = KC * QT * 4 / W;
+      unsigned s[kS], w[kL][QB];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int b = (first + st + j) * 4 + g;
-            v |= (b < nb ? p.q.scales[q * nb + b] : 127u) << (8 * j);
-          }
-        }
-        lds_s[f * 64 + lane] = v;
+      for (int i = 0; i < kL; ++i) {  // part h (four queries) of query tile qt of set st
+        const int f = wave + W * i, st = min(first + f / (QT * 4), sets - 1), qt = f / 4 % QT, h = f % 4;
+        const unsigned q = min(q0 + qt * 16 + h * 4 + g, last_q);
+        const int blk = st * 16 + (st == sets - 1 ? min(end_steps * b4 + min(c4, end_steps - 1), end_blocks - 1) : r16);
+        load_block<QB>(w[i], p.q.codes + ((unsigned long long)q * nb + blk) * (4 * QB));
       }
+#pragma unroll
+      for (int i = 0; i < kS; ++i) {
+        const int f = min(wave + W * i, have * QT - 1), st = first + f / QT, qt = f % QT;
+        const int from = (st == sets - 1 ? end_steps : 4) * g, in = min((st == sets - 1 ? end_blocks : 16) - from, 4);
+        const unsigned long long at = (unsigned long long)min(q0 + qt * 16 + r16, last_q) * nb + st * 16;
+        s[i] = first_bytes(load_bytes(p.q.scales + at + (in > 0 ? from : 0), max(in, 1)), in);
+      }
+#pragma unroll
+      for (int i = 0; i < kL; ++i) {
+        const int f = wave + W * i, q = f % 4 * 4 + g;  // query within its tile
+        if (f < have * QT * 4) {
+          const int to = (f / 4 * 16 + q) * 16 + (r16 ^ q);
+          lds_lo[to] = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+          if constexpr (QB == 6) lds_hi[to] = make_uint2(w[i][4], w[i][5]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kS; ++i)
+        if (wave + W * i < have * QT) lds_s[(wave + W * i) * 64 + lane] = s[i];
       __syncthreads();
     };
 
-    // The row of subtile t that this lane loads, within the tile.
+    auto first_row = [&](long long tile) { return TAIL ? tile * ROWS : min(tile * ROWS, p.r.rows - ROWS); };
     auto load = [&](RowSet<RB, RT>& a, long long tile, int set) {
-      const long long base = tile * (64 * RT);
-      const unsigned char* codes = p.r.codes + base * row_bytes;
-      const unsigned char* scales = p.r.scales + base * nb;
-      const int last = (int)min(p.r.rows - base, 64ll * RT) - 1;
+      const long long row0 = first_row(tile) + wave * (16 * RT);
+      const unsigned char* codes = p.r.codes + row0 * row_bytes + set * (64 * RB);
+      const unsigned char* scales = p.r.scales + row0 * nb;
+      const bool end = set == sets - 1;
+      const int blk = end ? min(end_steps * g + min(c4, end_steps - 1), end_blocks - 1) : 4 * g + c4;
+      const unsigned at = (unsigned)(group * b4) * row_bytes + (unsigned)blk * (4 * RB);
+      const unsigned from = (unsigned)(group * b4 + c4) * nb + set * 16 + (end ? end_steps : 4) * g;
+      const unsigned bytes = (unsigned)min((p.r.rows - row0) * nb, 0x7fffffffll);
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        const int row = min(wave * 16 * RT + 4 * RT * (r16 >> 2) + 4 * t + (r16 & 3), last);
+        if constexpr (TAIL) {
+          const int most = (int)(p.r.rows - row0) - 1;  // may be below 0
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int step = set * 4 + j, b = step * 4 + g;
-          if (step < steps) {
-            const int bc = min(b, nb - 1);
-            a.c[t][j].load(codes + (unsigned)row * (unsigned)row_bytes + (unsigned)bc * (4 * RB));
-            const unsigned s = scales[(unsigned)row * (unsigned)nb + (unsigned)bc];
-            a.s[t][j] = b < nb ? s : 127u;  // the queries are zero there
-          }
+          for (int i = 0; i < 4; ++i)
+            load_block<RB>(a.w[t][i], codes + (long long)min(group * b4 + subtile(t) + i, most) * row_bytes + blk * (4 * RB));
+          const long long s0 = (long long)min(group * b4 + c4 + subtile(t), most) * nb + set * 16;
+          const int n = end ? end_steps : 4;
+          a.s[t] = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            a.s[t] |= (unsigned)scales[s0 + min(n * g + j, (end ? end_blocks : 16) - 1)] << (8 * j);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) load_block<RB>(a.w[t][i], codes + (at + (unsigned)(subtile(t) + i) * row_bytes));
+          a.s[t] = load_scales(scales, from + subtile(t) * nb, bytes);
         }
       }
     };
 
     f32x4 acc[RT][QT];
-    auto clear = [&] {
+    auto product = [&](RowSet<RB, RT>& a, int set) {
+      const int at = set % KC, steps = set == sets - 1 ? end_steps : 4;
+      const int in = set == sets - 1 ? end_blocks - end_steps * g : 4;
 #pragma unroll
-      for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int j = 0; j < QT; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    };
-    auto product = [&](const RowSet<RB, RT>& a, int set) {
-      const int at = set % (KC / 4);
+      for (int t = 0; t < RT; ++t) {
+        transpose4<RB>(a.w[t], c4 & 1, c4 & 2);
+        a.s[t] = first_bytes(a.s[t], in);
+      }
       unsigned sb[QT];
 #pragma unroll
       for (int j = 0; j < QT; ++j) sb[j] = lds_s[(at * QT + j) * 64 + lane];
       auto one = [&](auto st) {
         constexpr int s = decltype(st)::value;
-        if (set * 4 + s >= steps) return;
 #pragma unroll
         for (int j = 0; j < QT; ++j) {
-          Codes<QB> b;
-          const int f = ((at * 4 + s) * QT + j) * 64 + lane;
+          const int f = ((at * QT + j) * 16 + r16) * 16 + ((4 * g + s) ^ r16);
+          unsigned b[QB];
           const uint4 lo = lds_lo[f];
-          b.w[0] = lo.x, b.w[1] = lo.y, b.w[2] = lo.z, b.w[3] = lo.w;
+          b[0] = lo.x, b[1] = lo.y, b[2] = lo.z, b[3] = lo.w;
           if constexpr (QB == 6) {
             const uint2 hi = lds_hi[f];
-            b.w[4] = hi.x, b.w[5] = hi.y;
+            b[4] = hi.x, b[5] = hi.y;
           }
 #pragma unroll
-          for (int t = 0; t < RT; ++t) acc[t][j] = mfma_mx<RB, QB, s>(a.c[t][s], a.s[t][s], b, sb[j], acc[t][j]);
+          for (int t = 0; t < RT; ++t) acc[t][j] = mfma_mx<RB, QB, s>(a.w[t][s], a.s[t], b, sb[j], acc[t][j]);
         }
       };
       one(std::integral_constant<int, 0>{});
-      one(std::integral_constant<int, 1>{});
-      one(std::integral_constant<int, 2>{});
-      one(std::integral_constant<int, 3>{});
+      if (steps > 1) one(std::integral_constant<int, 1>{});
+      if (steps > 2) one(std::integral_constant<int, 2>{});
+      if (steps > 3) one(std::integral_constant<int, 3>{});
     };
     auto store = [&](long long tile) {
-      const long long row = tile * (64 * RT) + wave * 16 * RT + 4 * RT * g;
-      const long long left = p.r.rows - row;
+      const long long row = first_row(tile) + wave * (16 * RT);
 #pragma unroll
       for (int j = 0; j < QT; ++j) {
-        const long long q = q0 + j * 16 + r16;
-        if (q >= p.q.rows) continue;
-        float v[4 * RT];
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[4 * t + i] = acc[t][j][i];
+        const unsigned q = q0 + j * 16 + r16;
+        if (q > last_q) continue;
         const long long at = q * p.ld + row;
-        if (p.dtype == kDtypeF32)
-          store_rows(static_cast<float*>(p.out) + at, v, left);
-        else if (p.dtype == kDtypeBF16)
-          store_rows(static_cast<__bf16*>(p.out) + at, v, left);
-        else
-          store_rows(static_cast<_Float16*>(p.out) + at, v, left);
+        if (p.dtype != kDtypeF32) {
+          constexpr int N = RT > 1 ? 8 : 4;
+#pragma unroll
+          for (int h = 0; h < 4 * RT / N; ++h) {
+            float v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = acc[h * (N / 4) + i / 4][j][i % 4];
+            const int in = 4 * N * h + N * g;
+            if (p.dtype == kDtypeBF16)
+              store_rows<TAIL>(static_cast<__bf16*>(p.out) + at + in, v, p.r.rows - row - in);
+            else
+              store_rows<TAIL>(static_cast<_Float16*>(p.out) + at + in, v, p.r.rows - row - in);
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            const float v[4] = {acc[t][j][0], acc[t][j][1], acc[t][j][2], acc[t][j][3]};
+            store_rows<TAIL>(static_cast<float*>(p.out) + at + 16 * t + 4 * g, v, p.r.rows - row - 16 * t - 4 * g);
+          }
+        }
       }
     };
 
-    const bool resident = steps <= KC;
+    // Sets of all tiles one after the other, each loaded while the one before it is multiplied.
     long long tile = t0, next_tile = t0;
     int set = 0, next_set = 0;
-    RowSet<RB, RT> a, b;
-    auto advance = [&] {
-      if (++next_set == sets) next_set = 0, ++next_tile;
-    };
+    RowSet<RB, RT> x, y;
     auto turn = [&](RowSet<RB, RT>& cur, RowSet<RB, RT>& next) {
-      if (set == 0) clear();
-      if (!resident && set % (KC / 4) == 0) stage(set * 4);
-      advance();
-      if (next_tile < t1) load(next, next_tile, next_set);
+      if (set == 0) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int j = 0; j < QT; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      if (!RES && set % KC == 0) stage(set);
+      if (++next_set == sets) next_set = 0, next_tile = min(next_tile + 1, t1 - 1);  // past the end: loaded, not used
+      load(next, next_tile, next_set);
+      __builtin_amdgcn_sched_barrier(0);
       product(cur, set);
-      if (set == sets - 1) store(tile);
-      tile = next_tile, set = next_set;
+      if (++set == sets) {
+        store(tile);
+        set = 0;
+        ++tile;
+      }
     };
-    if (tile < t1) load(a, tile, 0);
-    if (resident) stage(0);
-    while (tile < t1) {
-      turn(a, b);
+    load(x, tile, 0);
+    if constexpr (RES) stage(0);
+    for (;;) {
+      turn(x, y);
       if (tile >= t1) break;
-      turn(b, a);
+      turn(y, x);
+      if (tile >= t1) break;
     }
   }
 }
 
-template <int QB, int RB, int RT, int QT>
+template <int QB, int RB, int W, int RT, int QT, bool RES, bool TAIL = false>
 hipError_t launch(ScoresArgs p, hipStream_t s) {
   p.n_qblocks = (int)((p.q.rows + 16 * QT - 1) / (16 * QT));
-  p.tiles = (p.r.rows + 64 * RT - 1) / (64 * RT);
-  p.n_chunks = (int)std::max<long long>(1, std::min<long long>(p.tiles, 512 / std::min(p.n_qblocks, 512)));
+  const int tiles = (int)((p.r.rows + W * RT * 16 - 1) / (W * RT * 16));
+  // Eight waves per CU.
+  const int most = 2048 / W;
+  p.n_chunks = std::max(1, std::min(tiles, most / std::min(p.n_qblocks, most)));
+  p.least = tiles / p.n_chunks;
+  p.spare = tiles % p.n_chunks;
   const long long items = (long long)p.n_qblocks * p.n_chunks;
-  const int kc = std::min(lds_steps<QT>(), (p.r.nb + 15) / 16 * 4);
-  const unsigned lds = (unsigned)(kc * QT * 64 * (4 * QB + 1));
-  scores_kernel<QB, RB, RT, QT><<<(unsigned)std::min<long long>(items, 1 << 20), 256, lds, s>>>(p);
+  const int kc = std::min(lds_sets<QT>(), (p.r.nb + 15) / 16);
+  const unsigned lds = (unsigned)(kc * QT * (256 * 4 * QB + 64 * 4));
+  scores_kernel<QB, RB, W, RT, QT, RES, TAIL><<<(unsigned)std::min<long long>(items, 1 << 20), W * 64, lds, s>>>(p);
   return hipGetLastError();
 }
 
@@ -255,11 +338,15 @@ hipError_t launch_mx_scores(const MxRows& q, const MxRows& rows, void* out, int 
   p.out = out;
   p.ld = ld;
   p.dtype = dtype;
+  const int sets = (q.nb + 15) / 16;
   return with_bits(q.bits, [&](auto qb) {
     return with_bits(rows.bits, [&](auto rb) {
-      if (q.rows <= 16) return launch<qb(), rb(), 1, 1>(p, s);
-      if (q.rows <= 64) return launch<qb(), rb(), 1, 4>(p, s);
-      return launch<qb(), rb(), 2, 8>(p, s);
+      constexpr int RT = rb() == 4 ? 2 : 1;  // (6 bits: a set of two subtiles takes too many registers)
+      if (rows.rows < 128) return launch<qb(), rb(), 8, 1, 4, false, true>(p, s);
+      if (q.rows <= 16 && sets <= lds_sets<1>()) return launch<qb(), rb(), 4, 1, 1, true>(p, s);
+      if (q.rows > 64 && sets <= lds_sets<8>() && rows.rows >= 128 * RT) return launch<qb(), rb(), 8, RT, 8, true>(p, s);
+      if (sets <= lds_sets<4>()) return launch<qb(), rb(), 8, 1, 4, true>(p, s);
+      return launch<qb(), rb(), 8, 1, 4, false>(p, s);
     });
   });
 }
