@@ -1,6 +1,21 @@
-// The gradient of the products of quantised rows (oprag_mx_scores_grad): G X or G^T X.
+// The gradient of the products of quantised rows (oprag_mx_scores_grad): out = G X, or G^T X.
+//
+// out[m, d] = sum over k of G(m, k) x^(k, d), x^ the values of the codes, as a matrix product on the bf16 matrix
+// instructions: a code's value has at most four significant bits, so it is a bf16 exactly (2^-130 at
+// the least), and an element of G is the sum of 1 (bf16), 2 (fp16) or 3 (fp32) bf16 planes of 8 bits
+// each, exactly too; their products with x^ all go to one fp32 sum.  (Two planes of fp32 would be
+// 2^-17 of each term off, fifty times what fp32 sums of a few hundred terms are.)
+//
+// A workgroup of eight waves makes BM rows x 256 dimensions of out, over a run of k, 64 at a time.
+// The threads load the stage after the next into registers (one block of codes each, and their share of
+// G), and decode, split and write the next one to the other half of LDS while this one is
+// multiplied.  Codes become [k][d]: the instruction wants eight k of one d in a lane, which the
+// transposing LDS read delivers; G stays [m][k], or, transposed, is [k][m] and read in the same way.
+// Few rows or columns of out leave most CUs without a tile: then k is split over workgroups, whose sums
+// go to the workspace and are added by a second kernel, in the order of k.
 #include <algorithm>
 
+#include "mfma.h"
 #include "mx.h"
 
 namespace oprag {
@@ -8,39 +23,376 @@ namespace {
 
 using namespace dev;
 
-// One thread per output element.
-template <int DT, int BITS>
-__global__ __launch_bounds__(256) void grad_kernel(const void* __restrict__ g, long long row_step, long long col_step,
-                                                   long long m, MxRows x, float* __restrict__ out, long long out_ld) {
-  const long long total = m * x.dim, stride = (long long)gridDim.x * 256;
-  for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < total; t += stride) {
-    const long long row = t / x.dim;
-    const int d = (int)(t - row * x.dim), bit = (d % 32) * BITS;
-    double sum = 0.0;  // a long index has more terms than fp32 adds exactly enough in a row
-    for (long long k = 0; k < x.rows; ++k) {
-      const long long b = k * x.nb + d / 32;
-      const unsigned char* p = x.codes + b * (4 * BITS) + bit / 8;
-      unsigned v = p[0] >> (bit % 8);
-      if (bit % 8 + BITS > 8) v |= (unsigned)p[1] << (8 - bit % 8);
-      sum += (double)load_as_f32<DT>(g, row * row_step + k * col_step) * (mx_decode<BITS>(v & ((1u << BITS) - 1)) * mx_scale(x.scales[b]));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x32 __attribute__((ext_vector_type(32)));
+typedef unsigned u32x6 __attribute__((ext_vector_type(6)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kBK = 64, kBD = 256, kThreads = 512;
+constexpr int kXBytes = kBK * kBD * 2;  // a stage's decoded rows
+
+struct GradArgs {
+  MxRows x;
+  const void* g;
+  long long ld, m;
+  float* out;
+  long long out_ld;
+  float* part;       // [splits][m][pitch], or null
+  long long pitch;
+  int m_tiles, d_tiles, splits;
+  int per;           // stages of a split
+};
+
+// 32-byte pieces of a [k][..] row lie at their place ^ mix(k): the 16 rows x 32 bytes of a transposing read
+// then touch every bank twice.
+__device__ __forceinline__ int mix(int k) { return (k & 3) | ((k >> 3) & 1) << 2; }
+
+template <int DT>
+constexpr int planes() {
+  return DT == kDtypeBF16 ? 1 : DT == kDtypeF16 ? 2 : 3;
+}
+
+// Two fp32 numbers as P planes of bf16 pairs (x low): each plane takes the upper half of the bits that are left.
+template <int P>
+__device__ __forceinline__ void split2(float x, float y, unsigned (&o)[P]) {
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const unsigned ux = __float_as_uint(x), uy = __float_as_uint(y);
+    o[i] = __builtin_amdgcn_perm(uy, ux, 0x07060302u);
+    if (i + 1 < P) {  // nothing is left of an infinity or a NaN
+      const float rx = x - __uint_as_float(ux & 0xffff0000u), ry = y - __uint_as_float(uy & 0xffff0000u);
+      x = rx == rx ? rx : 0.f;
+      y = ry == ry ? ry : 0.f;
     }
-    out[row * out_ld + d] = (float)sum;
   }
+}
+
+template <int DT>
+struct Elem;
+template <>
+struct Elem<kDtypeF32> { typedef float T; };
+template <>
+struct Elem<kDtypeBF16> { typedef unsigned short T; };
+template <>
+struct Elem<kDtypeF16> { typedef unsigned short T; };
+
+// EDGE: a transposed G with fewer columns than BM, read element by element.
+template <int DT, int BITS, bool TRANS, int BM, bool EDGE>
+__global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs p) {
+  using T = typename Elem<DT>::T;
+  constexpr int P = planes<DT>(), ES = sizeof(T), EV = 16 / ES;           // elements of a 16-byte load
+  constexpr int WM = BM == 128 ? 2 : 1, WD = 8 / WM;                      // wave grid
+  constexpr int MI = BM / WM / 16, DI = kBD / WD / 16;                    // a wave's subtiles
+  constexpr int kGBytes = BM * kBK * 2, kBuf = kXBytes + P * kGBytes;     // bytes of a plane, of a stage
+  constexpr int kChunks = BM * kBK / EV, kG = (kChunks + kThreads - 1) / kThreads;
+  constexpr int kRow = TRANS ? BM / EV : kBK / EV;                        // 16-byte loads per row of G's stage
+  constexpr int kMix = BM / 16 - 1;                                       // of a transposed G: its rows have BM / 16 pieces
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, g4 = lane >> 4;
+  const int wm = wave / WD, wd = wave % WD;
+
+  const unsigned L = (unsigned)logical_block();
+  const int di0 = (int)(L % p.d_tiles), mi0 = (int)(L / p.d_tiles % p.m_tiles), split = (int)(L / p.d_tiles / p.m_tiles);
+  // The last tile of a transposed G ends with its last column, and makes some rows of out that the tile before it has
+  // too, to the same bits.
+  const long long m0 = TRANS && !EDGE ? min((long long)mi0 * BM, p.m - BM) : (long long)mi0 * BM;
+  const int d0 = di0 * kBD;
+  const long long K = p.x.rows, k_first = (long long)split * p.per * kBK;
+  const int stages = (int)min((long long)p.per, (K - k_first + kBK - 1) / kBK);
+
+  // This thread's share of a stage: a block of codes and its scale, and kG pieces of G.
+  struct Share {
+    unsigned c[BITS], s;
+    u32x4 g[kG];
+  };
+  typedef T V __attribute__((ext_vector_type(EV), aligned(ES)));
+  const int xk = tid >> 3, xb = d0 / 32 + (tid & 7);
+  const bool x_in = xb < p.x.nb;
+  const long long x_at = (k_first + xk) * p.x.nb + min(xb, p.x.nb - 1);
+  auto load_codes = [&](Share& a, long long b) {
+    typedef unsigned V4 __attribute__((ext_vector_type(4), aligned(8)));
+    typedef unsigned V2 __attribute__((ext_vector_type(2), aligned(8)));
+    const unsigned char* c = p.x.codes + b * (4 * BITS);
+    const V4 lo = *reinterpret_cast<const V4*>(c);
+    a.c[0] = lo[0], a.c[1] = lo[1], a.c[2] = lo[2], a.c[3] = lo[3];
+    if constexpr (BITS == 6) {
+      const V2 hi = *reinterpret_cast<const V2*>(c + 16);
+      a.c[4] = hi[0], a.c[5] = hi[1];
+    }
+    a.s = p.x.scales[b];
+  };
+  // Piece i of G: its row and column in the stage.  Rows past m are read from the last one and not stored.
+  auto piece = [&](int i) { return min(tid + i * kThreads, kChunks - 1); };
+  const T* g_at[kG];
+#pragma unroll
+  for (int i = 0; i < kG; ++i) {
+    const int row = piece(i) / kRow, col = piece(i) % kRow * EV;
+    g_at[i] = static_cast<const T*>(p.g) +
+              (TRANS ? (k_first + row) * p.ld + m0 + col : min(m0 + row, p.m - 1) * p.ld + k_first + col);
+  }
+  const long long g_step = TRANS ? kBK * p.ld : kBK;
+  auto load_whole = [&](Share& a, int stage) {  // a stage with all its k
+    load_codes(a, x_at + (long long)stage * kBK * p.x.nb);
+#pragma unroll
+    for (int i = 0; i < kG; ++i) a.g[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const V*>(g_at[i] + stage * g_step));
+    __builtin_amdgcn_sched_barrier(0);  // loads stay in their order: the wait for one leaves those after it in flight
+  };
+  auto load_some = [&](Share& a, int stage) {
+    const long long k0 = k_first + (long long)stage * kBK;
+#pragma unroll
+    for (int i = 0; i < BITS; ++i) a.c[i] = 0u;
+    a.s = 127u;
+    if (k0 + xk < K) load_codes(a, x_at + (long long)stage * kBK * p.x.nb);
+#pragma unroll
+    for (int i = 0; i < kG; ++i) {
+      const int row = piece(i) / kRow, col = piece(i) % kRow * EV;
+      const long long in = TRANS ? (k0 + row < K ? p.m - m0 - col : 0) : K - k0 - col;
+      V v;
+#pragma unroll
+      for (int e = 0; e < EV; ++e) v[e] = e < in ? g_at[i][stage * g_step + e] : (T)0;
+      a.g[i] = __builtin_bit_cast(u32x4, v);
+    }
+  };
+
+  auto write = [&](const Share& a, unsigned char* buf) {
+    const float scale = __uint_as_float(a.s == 0u ? 0x00400000u : a.s << 23);  // (255: infinite, which makes NaN)
+    unsigned v[16];
+    if constexpr (BITS == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[4 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a.c[i], scale, 0));
+        v[4 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a.c[i], scale, 1));
+        v[4 * i + 2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a.c[i], scale, 2));
+        v[4 * i + 3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a.c[i], scale, 3));
+      }
+    } else {
+      const u32x6 c = {a.c[0], a.c[1], a.c[2], a.c[3], a.c[4], a.c[5]};
+      const bf16x32 t = __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(c, scale);
+      __builtin_memcpy(v, &t, 64);
+    }
+    if (!x_in) {  // past the row's end: not stored, but no NaN to slow anything down either
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = 0u;
+    }
+    unsigned char* row = buf + xk * (kBD * 2);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4* to = reinterpret_cast<u32x4*>(row + ((2 * (tid & 7) + h) ^ mix(xk)) * 32);
+      to[0] = u32x4{v[8 * h], v[8 * h + 1], v[8 * h + 2], v[8 * h + 3]};
+      to[1] = u32x4{v[8 * h + 4], v[8 * h + 5], v[8 * h + 6], v[8 * h + 7]};
+    }
+    unsigned char* gb = buf + kXBytes;
+#pragma unroll
+    for (int i = 0; i < kG; ++i) {
+      const int row = piece(i) / kRow, col = piece(i) % kRow * EV;
+      // Byte of the piece in a plane: [k][m] as the codes, or [m][k] in 16-byte pieces, piece c of row m at c ^ (m / 2).
+      const int at = TRANS ? row * (BM * 2) + ((col / 16) ^ (mix(row) & kMix)) * 32 + col % 16 * 2
+                           : row * (kBK * 2) + ((col / 8) ^ ((row >> 1) & 7)) * 16 + col % 8 * 2;
+      if constexpr (DT == kDtypeBF16) {
+        *reinterpret_cast<u32x4*>(gb + at) = a.g[i];
+      } else if constexpr (DT == kDtypeF16) {
+        unsigned o[4][P];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+          const unsigned pair = a.g[i][e];
+          const h2 h = __builtin_bit_cast(h2, pair);
+          split2<P>((float)h[0], (float)h[1], o[e]);
+        }
+#pragma unroll
+        for (int pl = 0; pl < P; ++pl)
+          *reinterpret_cast<u32x4*>(gb + pl * kGBytes + at) = u32x4{o[0][pl], o[1][pl], o[2][pl], o[3][pl]};
+      } else {
+        unsigned o[2][P];
+        split2<P>(__uint_as_float(a.g[i][0]), __uint_as_float(a.g[i][1]), o[0]);
+        split2<P>(__uint_as_float(a.g[i][2]), __uint_as_float(a.g[i][3]), o[1]);
+#pragma unroll
+        for (int pl = 0; pl < P; ++pl) *reinterpret_cast<u32x2*>(gb + pl * kGBytes + at) = u32x2{o[0][pl], o[1][pl]};
+      }
+    }
+  };
+
+  // Four k of one column for every lane: rows r, .. r + 3 of a [k][..] array, 16 columns, lane i of 16 takes column i.
+  auto tr_read = [&](const unsigned char* at) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)at);
+  };
+  const int tr_row = 8 * g4 + (r16 >> 2), tr_mix = mix(tr_row), tr_col = (r16 & 3) * 8;
+  f32x4 acc[DI][MI];
+#pragma unroll
+  for (int i = 0; i < DI; ++i)
+#pragma unroll
+    for (int j = 0; j < MI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto product = [&](const unsigned char* buf) {
+#pragma unroll
+    for (int ks = 0; ks < kBK / 32; ++ks) {
+      bf16x8 xf[DI];
+#pragma unroll
+      for (int i = 0; i < DI; ++i) {
+        const unsigned char* at = buf + (ks * 32 + tr_row) * (kBD * 2) + ((wd * DI + i) ^ tr_mix) * 32 + tr_col;
+        const bf16x4 a = tr_read(at), b = tr_read(at + 4 * (kBD * 2));
+        xf[i] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+#pragma unroll
+      for (int pl = 0; pl < P; ++pl) {
+        const unsigned char* gb = buf + kXBytes + pl * kGBytes;
+#pragma unroll
+        for (int j = 0; j < MI; ++j) {
+          bf16x8 gf;
+          if constexpr (TRANS) {
+            const unsigned char* at =
+                gb + (ks * 32 + tr_row) * (BM * 2) + ((wm * MI + j) ^ (tr_mix & kMix)) * 32 + tr_col;
+            const bf16x4 a = tr_read(at), b = tr_read(at + 4 * (BM * 2));
+            gf = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+          } else {
+            const int m = (wm * MI + j) * 16 + r16;
+            gf = *reinterpret_cast<const bf16x8*>(gb + m * (kBK * 2) + ((ks * 4 + g4) ^ ((m >> 1) & 7)) * 16);
+          }
+#pragma unroll
+          for (int i = 0; i < DI; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[i], gf, acc[i][j], 0, 0, 0);
+        }
+      }
+    }
+  };
+
+  // Stage s is multiplied from half s % 2 of LDS while stage s + 1 is written and stage s + 2 loaded.  A
+  // last stage without all its k is on its own.
+  const int whole = EDGE ? 0 : (int)min((long long)stages, (K - k_first) / kBK);
+  Share a, b;
+  if (whole > 0) {
+    load_whole(a, 0);
+    load_whole(b, min(1, whole - 1));
+    write(a, smem);
+    lds_barrier();
+    for (int s = 0;;) {
+      load_whole(a, min(s + 2, whole - 1));  // past the end: loaded, not used
+      write(b, smem + kBuf);
+      product(smem);
+      lds_barrier();
+      if (++s >= whole) break;
+      load_whole(b, min(s + 2, whole - 1));
+      write(a, smem);
+      product(smem + kBuf);
+      lds_barrier();
+      if (++s >= whole) break;
+    }
+  }
+  for (int s = whole; s < stages; ++s) {
+    load_some(a, s);
+    write(a, smem);
+    lds_barrier();
+    product(smem);
+    lds_barrier();
+  }
+
+  float* out = p.part ? p.part + (long long)split * p.m * p.pitch : p.out;
+  const long long ld = p.part ? p.pitch : p.out_ld;
+#pragma unroll
+  for (int j = 0; j < MI; ++j) {
+    const long long m = m0 + (wm * MI + j) * 16 + r16;
+    if (m >= p.m) continue;
+#pragma unroll
+    for (int i = 0; i < DI; ++i) {
+      const int d = d0 + (wd * DI + i) * 16 + 4 * g4;
+      float* to = out + m * ld + d;
+      typedef float V __attribute__((ext_vector_type(4), aligned(4)));
+      if (d + 4 <= p.x.dim) {
+        *reinterpret_cast<V*>(to) = acc[i][j];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (d + e < p.x.dim) to[e] = acc[i][j][e];
+      }
+    }
+  }
+}
+
+// out[m, d] = the sum of the splits' sums, in their order (0 without a split).
+__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, long long m, int dim, long long pitch,
+                                                   int splits, float* __restrict__ out, long long out_ld) {
+  const long long quads = pitch / 4, total = m * quads, stride = (long long)gridDim.x * 256;
+  for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < total; t += stride) {
+    const long long row = t / quads;
+    const int d = (int)(t - row * quads) * 4;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    const f32x4* from = reinterpret_cast<const f32x4*>(part + row * pitch + d);
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) sum += from[(long long)s * total];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (d + e < dim) out[row * out_ld + d + e] = sum[e];
+  }
+}
+
+struct GradPlan {
+  int bm, m_tiles, d_tiles, splits, per;
+};
+GradPlan plan_grad(long long m, const MxRows& x) {
+  GradPlan p;
+  p.bm = m <= 16 ? 16 : m <= 64 ? 64 : 128;
+  p.m_tiles = (int)((m + p.bm - 1) / p.bm);
+  p.d_tiles = (x.dim + kBD - 1) / kBD;
+  const long long stages = (x.rows + kBK - 1) / kBK, tiles = (long long)p.m_tiles * p.d_tiles;
+  // A workgroup per CU (two where the tile is small), of four stages or more.
+  const long long most = std::max<long long>(1, (p.bm == 16 ? 512 : 256) / tiles);
+  p.per = (int)std::max<long long>((stages + most - 1) / most, std::min<long long>(stages, 4));
+  p.splits = p.per ? (int)((stages + p.per - 1) / p.per) : 0;
+  return p;
+}
+long long part_pitch(const MxRows& x) { return (x.dim + 3) & ~3; }
+
+template <int DT, int BITS, bool TRANS, int BM, bool EDGE>
+hipError_t launch_tiles(const GradArgs& a, hipStream_t s) {
+  constexpr unsigned lds = 2 * (kXBytes + planes<DT>() * BM * kBK * 2);
+  static_assert(lds <= 163840, "LDS");
+  const long long grid = (long long)a.m_tiles * a.d_tiles * a.splits;
+  grad_kernel<DT, BITS, TRANS, BM, EDGE><<<(unsigned)grid, kThreads, lds, s>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t mx_grad_workspace_bytes(long long, const MxRows&) { return 0; }
+size_t mx_grad_workspace_bytes(long long m, const MxRows& x) {
+  const GradPlan p = plan_grad(m, x);
+  return p.splits > 1 ? (size_t)p.splits * (size_t)m * (size_t)part_pitch(x) * 4 : 0;
+}
 
 hipError_t launch_mx_grad(const void* grad, int dtype, long long ld, bool transposed, long long m, const MxRows& x,
-                          float* out, long long out_ld, void*, hipStream_t s) {
-  const unsigned grid = (unsigned)std::min<long long>((m * x.dim + 255) / 256, 1 << 16);
-  return with_dtype(dtype, [&](auto dt) {
-    return with_bits(x.bits, [&](auto bits) {
-      grad_kernel<dt(), bits()><<<grid, 256, 0, s>>>(grad, transposed ? 1 : ld, transposed ? ld : 1, m, x, out, out_ld);
-      return hipGetLastError();
+                          float* out, long long out_ld, void* ws, hipStream_t s) {
+  const GradPlan p = plan_grad(m, x);
+  GradArgs a;
+  a.x = x;
+  a.g = grad;
+  a.ld = ld;
+  a.m = m;
+  a.out = out;
+  a.out_ld = out_ld;
+  a.part = p.splits > 1 ? static_cast<float*>(ws) : nullptr;
+  a.pitch = part_pitch(x);
+  a.m_tiles = p.m_tiles;
+  a.d_tiles = p.d_tiles;
+  a.splits = p.splits;
+  a.per = p.per;
+  if (p.splits > 0) {
+    const hipError_t e = with_dtype(dtype, [&](auto dt) {
+      return with_bits(x.bits, [&](auto bits) {
+        auto go = [&](auto bm) {
+          if (!transposed) return launch_tiles<dt(), bits(), false, bm(), false>(a, s);
+          if (m < bm()) return launch_tiles<dt(), bits(), true, bm(), true>(a, s);
+          return launch_tiles<dt(), bits(), true, bm(), false>(a, s);
+        };
+        if (p.bm == 16) return go(std::integral_constant<int, 16>{});
+        if (p.bm == 64) return go(std::integral_constant<int, 64>{});
+        return go(std::integral_constant<int, 128>{});
+      });
     });
-  });
+    if (e != hipSuccess || p.splits == 1) return e;
+  }
+  const long long quads = m * (a.pitch / 4);
+  join_kernel<<<(unsigned)std::min<long long>((quads + 255) / 256, 4096), 256, 0, s>>>(a.part, m, x.dim, a.pitch, p.splits, out,
+                                                                                      out_ld);
+  return hipGetLastError();
 }
 
 }  // namespace oprag
