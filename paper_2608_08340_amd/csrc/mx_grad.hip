@@ -12,7 +12,10 @@
 // multiplied.  Codes become [k][d]: the instruction wants eight k of one d in a lane, which the
 // transposing LDS read delivers; G stays [m][k], or, transposed, is [k][m] and read in the same way.
 // Few rows or columns of out leave most CUs without a tile: then k is split over workgroups, whose sums
-// go to the workspace and are added by a second kernel, in the order of k.
+// go to the workspace and are added by a second kernel, in a fixed order.
+//
+// Up to kFew rows of out: no matrix instruction, which would be mostly idle while codes take the way
+// through LDS.  A thread owns a block of 32 dimensions, decodes it to fp32 and adds G's multiples.
 #include <algorithm>
 
 #include "mfma.h"
@@ -150,8 +153,12 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs p) {
       const int row = piece(i) / kRow, col = piece(i) % kRow * EV;
       const long long in = TRANS ? (k0 + row < K ? p.m - m0 - col : 0) : K - k0 - col;
       V v;
+      if (in >= EV) {
+        v = *reinterpret_cast<const V*>(g_at[i] + stage * g_step);
+      } else {
 #pragma unroll
-      for (int e = 0; e < EV; ++e) v[e] = e < in ? g_at[i][stage * g_step + e] : (T)0;
+        for (int e = 0; e < EV; ++e) v[e] = e < in ? g_at[i][stage * g_step + e] : (T)0;
+      }
       a.g[i] = __builtin_bit_cast(u32x4, v);
     }
   };
@@ -179,7 +186,7 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs p) {
     unsigned char* row = buf + xk * (kBD * 2);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      u32x4* to = reinterpret_cast<u32x4*>(row + ((2 * (tid & 7) + h) ^ mix(xk)) * 32);
+      u32x4* to = reinterpret_cast<u32x4*>(row + ((2 * (tid & 7) + h) ^ mix(xk) ^ ((tid >> 2) & 1)) * 32);
       to[0] = u32x4{v[8 * h], v[8 * h + 1], v[8 * h + 2], v[8 * h + 3]};
       to[1] = u32x4{v[8 * h + 4], v[8 * h + 5], v[8 * h + 6], v[8 * h + 7]};
     }
@@ -230,7 +237,7 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs p) {
       bf16x8 xf[DI];
 #pragma unroll
       for (int i = 0; i < DI; ++i) {
-        const unsigned char* at = buf + (ks * 32 + tr_row) * (kBD * 2) + ((wd * DI + i) ^ tr_mix) * 32 + tr_col;
+        const unsigned char* at = buf + (ks * 32 + tr_row) * (kBD * 2) + ((wd * DI + i) ^ tr_mix ^ ((wd * DI + i) >> 3)) * 32 + tr_col;
         const bf16x4 a = tr_read(at), b = tr_read(at + 4 * (kBD * 2));
         xf[i] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
       }
@@ -308,20 +315,136 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs p) {
   }
 }
 
-// out[m, d] = the sum of the splits' sums, in their order (0 without a split).
+// Few rows of out: M of them.  Thread t takes block t % nb (nb <= kFewThreads) of every (kFewThreads / nb)-th k of
+// the split's run; the threads of a block add up through LDS.
+constexpr int kFew = 4, kFewThreads = 256;
+template <int DT, int BITS, int M>
+__global__ __launch_bounds__(kFewThreads) void few_kernel(GradArgs p, long long m_step, long long k_step) {
+  __shared__ float sums[kFewThreads * 33];
+  const int nb = p.x.nb, groups = kFewThreads / nb, tid = threadIdx.x, blk = tid % nb, group = tid / nb;
+  const long long k0 = (long long)blockIdx.x * p.per, k1 = min(k0 + p.per, p.x.rows);
+  float acc[M][32];
+#pragma unroll
+  for (int m = 0; m < M; ++m)
+#pragma unroll
+    for (int i = 0; i < 32; ++i) acc[m][i] = 0.f;
+  if (group < groups) {
+    // kDeep rows' loads in flight, the rest of the run one row after the other
+    constexpr int kDeep = 4;
+    struct Row {
+      unsigned c[BITS], s;
+      typename Elem<DT>::T g[M];
+    };
+    auto load = [&](Row& r, long long k) {
+      const long long b = k * nb + blk;
+      typedef unsigned V4 __attribute__((ext_vector_type(4), aligned(8)));
+      typedef unsigned V2 __attribute__((ext_vector_type(2), aligned(8)));
+      const V4 lo = *reinterpret_cast<const V4*>(p.x.codes + b * (4 * BITS));
+      r.c[0] = lo[0], r.c[1] = lo[1], r.c[2] = lo[2], r.c[3] = lo[3];
+      if constexpr (BITS == 6) {
+        const V2 hi = *reinterpret_cast<const V2*>(p.x.codes + b * (4 * BITS) + 16);
+        r.c[4] = hi[0], r.c[5] = hi[1];
+      }
+      r.s = p.x.scales[b];
+#pragma unroll
+      for (int m = 0; m < M; ++m) r.g[m] = static_cast<const typename Elem<DT>::T*>(p.g)[min((long long)m, p.m - 1) * m_step + k * k_step];
+    };
+    auto add = [&](const Row& r) {
+      const float scale = __uint_as_float(r.s == 0u ? 0x00400000u : r.s << 23);
+      float v[32];
+      if constexpr (BITS == 4) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(r.c[i], scale, 0);
+          const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(r.c[i], scale, 1);
+          const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(r.c[i], scale, 2);
+          const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(r.c[i], scale, 3);
+          v[8 * i] = a[0], v[8 * i + 1] = a[1], v[8 * i + 2] = b[0], v[8 * i + 3] = b[1];
+          v[8 * i + 4] = c[0], v[8 * i + 5] = c[1], v[8 * i + 6] = d[0], v[8 * i + 7] = d[1];
+        }
+      } else {
+        const u32x6 c = {r.c[0], r.c[1], r.c[2], r.c[3], r.c[4], r.c[5]};
+        const auto t = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(c, scale);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = t[i];
+      }
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        const float g = load_as_f32<DT>(&r.g[m], 0);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) acc[m][i] = fmaf(g, v[i], acc[m][i]);
+      }
+    };
+    long long k = k0 + group;
+    const long long step = groups;
+    Row r[kDeep];
+    if (k + (kDeep - 1) * step < k1) {
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) load(r[i], k + i * step);
+      for (k += kDeep * step; k + (kDeep - 1) * step < k1; k += kDeep * step) {
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+          add(r[i]);
+          load(r[i], k + i * step);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) add(r[i]);
+    }
+    for (; k < k1; k += step) {
+      load(r[0], k);
+      add(r[0]);
+    }
+  }
+  float* out = p.part ? p.part + (long long)blockIdx.x * p.m * p.pitch : p.out;
+  const long long ld = p.part ? p.pitch : p.out_ld;
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    if (m >= p.m) break;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sums[tid * 33 + i] = acc[m][i];  // (33: neighbours' elements in different banks)
+    __syncthreads();
+    for (int d = tid; d < p.x.dim; d += kFewThreads) {
+      const float* from = sums + d / 32 * 33 + d % 32;
+      float v = from[0];
+      for (int g = 1; g < groups; ++g) v += from[g * nb * 33];
+      out[m * ld + d] = v;
+    }
+  }
+}
+
+// out[m, d] = the sum of the splits' sums (0 without a split): LANES threads of an element each add every
+// LANES-th split, and then their sums are added in order.
+template <int LANES>
 __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, long long m, int dim, long long pitch,
                                                    int splits, float* __restrict__ out, long long out_ld) {
-  const long long quads = pitch / 4, total = m * quads, stride = (long long)gridDim.x * 256;
-  for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < total; t += stride) {
-    const long long row = t / quads;
-    const int d = (int)(t - row * quads) * 4;
+  constexpr int kAt = 256 / LANES;
+  __shared__ f32x4 sums[LANES > 1 ? 256 : 1];
+  const int tid = threadIdx.x, lane = tid / kAt, at = tid % kAt;
+  const long long quads = pitch / 4, total = m * quads, stride = (long long)gridDim.x * kAt;
+  for (long long t0 = (long long)blockIdx.x * kAt; t0 < total; t0 += stride) {
+    const long long t = min(t0 + at, total - 1);
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    const f32x4* from = reinterpret_cast<const f32x4*>(part + row * pitch + d);
+    const f32x4* from = reinterpret_cast<const f32x4*>(part) + t;
 #pragma unroll 8
-    for (int s = 0; s < splits; ++s) sum += from[(long long)s * total];
+    for (int s = lane; s < splits; s += LANES) sum += from[(long long)s * total];
+    if constexpr (LANES > 1) {
+      __syncthreads();
+      sums[tid] = sum;
+      __syncthreads();
+    }
+    if (lane == 0 && t0 + at < total) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (d + e < dim) out[row * out_ld + d + e] = sum[e];
+      for (int i = 1; i < LANES; ++i) sum += sums[i * kAt + at];
+      const long long row = t / quads;
+      const int d = (int)(t - row * quads) * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (d + e < dim) out[row * out_ld + d + e] = sum[e];
+    }
   }
 }
 
@@ -330,6 +453,14 @@ struct GradPlan {
 };
 GradPlan plan_grad(long long m, const MxRows& x) {
   GradPlan p;
+  if (m <= kFew && x.nb <= kFewThreads) {  // per: k of a workgroup, eight or more of every thread
+    p.bm = 0;
+    p.m_tiles = p.d_tiles = 1;
+    const long long least = 8 * (kFewThreads / x.nb);
+    p.per = (int)std::min<long long>(std::max<long long>((x.rows + 1023) / 1024, least), std::max<long long>(x.rows, 1));
+    p.splits = (int)((x.rows + p.per - 1) / p.per);
+    return p;
+  }
   p.bm = m <= 16 ? 16 : m <= 64 ? 64 : 128;
   p.m_tiles = (int)((m + p.bm - 1) / p.bm);
   p.d_tiles = (x.dim + kBD - 1) / kBD;
@@ -382,6 +513,15 @@ hipError_t launch_mx_grad(const void* grad, int dtype, long long ld, bool transp
           if (m < bm()) return launch_tiles<dt(), bits(), true, bm(), true>(a, s);
           return launch_tiles<dt(), bits(), true, bm(), false>(a, s);
         };
+        if (p.bm == 0) {
+          auto few = [&](auto rows) {
+            few_kernel<dt(), bits(), rows()><<<(unsigned)p.splits, kFewThreads, 0, s>>>(a, transposed ? 1 : ld, transposed ? ld : 1);
+            return hipGetLastError();
+          };
+          if (m == 1) return few(std::integral_constant<int, 1>{});
+          if (m == 2) return few(std::integral_constant<int, 2>{});
+          return few(std::integral_constant<int, 4>{});
+        }
         if (p.bm == 16) return go(std::integral_constant<int, 16>{});
         if (p.bm == 64) return go(std::integral_constant<int, 64>{});
         return go(std::integral_constant<int, 128>{});
@@ -390,8 +530,18 @@ hipError_t launch_mx_grad(const void* grad, int dtype, long long ld, bool transp
     if (e != hipSuccess || p.splits == 1) return e;
   }
   const long long quads = m * (a.pitch / 4);
-  join_kernel<<<(unsigned)std::min<long long>((quads + 255) / 256, 4096), 256, 0, s>>>(a.part, m, x.dim, a.pitch, p.splits, out,
-                                                                                      out_ld);
+  auto join = [&](auto lanes) {
+    constexpr int kAt = 256 / lanes();
+    join_kernel<lanes()><<<(unsigned)std::min<long long>((quads + kAt - 1) / kAt, 4096), 256, 0, s>>>(
+        a.part, m, x.dim, a.pitch, p.splits, out, out_ld);
+  };
+  // Few elements: several threads each, or a handful of workgroups would add hundreds of splits.
+  if (quads >= 65536)
+    join(std::integral_constant<int, 1>{});
+  else if (quads >= 4096)
+    join(std::integral_constant<int, 8>{});
+  else
+    join(std::integral_constant<int, 32>{});
   return hipGetLastError();
 }
 
