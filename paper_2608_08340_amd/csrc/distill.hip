@@ -12,10 +12,15 @@
 // pieces of 8,192 over workgroups, each held in registers alike: one launch leaves every piece's
 // maximum, sum and share of sum p z in the workspace, a second joins them and, for the gradient,
 // reads the piece again.  A piece's gradient is stored densely; the list's entries on it are then
-// stored again by the threads that hold them, with their p taken off.
+// stored again, with their p taken off.
+//
+// Every workgroup has one wave more than its elements need: it makes the teacher (dependent loads and fp64
+// logarithms, about as long as the others take to load and reduce) and the loss, and stores the
+// entries.  (By a wave with elements of its own, before or after them: 1,024 x 32,768 fp32 89 us.)
 #include <algorithm>
 #include <cmath>
 
+#include "mfma.h"
 #include "mx.h"
 
 namespace oprag {
@@ -49,44 +54,42 @@ __device__ __forceinline__ float exp_diff(float d, const Args& p) {
   return __builtin_amdgcn_exp2f(fmaf(d, p.c_hi, d * p.c_lo));
 }
 
-// v becomes 2^((v - s_max) c); returns the sum.
+// v becomes 2^((v - s_ref) c); returns the sum.
 template <int N>
-__device__ __forceinline__ float exp_all(float (&v)[N], float s_max, const Args& p) {
+__device__ __forceinline__ float exp_all(float (&v)[N], float s_ref, const Args& p) {
   float s = 0.f;
-  if (s_max == kMinusInf) {  // nothing but -inf and NaN
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = v[i] != v[i] ? v[i] : 0.f;
-      s += v[i];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = exp_diff(v[i] - s_max, p);
-      s += v[i];
-    }
+  for (int i = 0; i < N; ++i) {
+    v[i] = exp_diff(v[i] - s_ref, p);
+    s += v[i];
+    if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // all differences at once would not fit
   }
   return s;
 }
+// What the differences are taken from: 0 for a row with nothing but -inf (and NaN).
+__device__ __forceinline__ float reference(float s_max) { return s_max == kMinusInf ? 0.f : s_max; }
 __device__ __forceinline__ float inverse(float s_max, float sum) { return s_max == kMinusInf && sum == sum ? 0.f : 1.f / sum; }
 
-// Reductions over a workgroup of T threads.  The caller leaves a barrier between two uses of `part`.
-template <int T>
-__device__ __forceinline__ float group_max(float v, float* part) {
+// Reductions over the T threads that hold elements, in two halves: what a wave leaves in `part`, and, past a barrier,
+// the whole (for the teacher's wave too).
+__device__ __forceinline__ void leave_max(float v, float* part) {
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = part[0];
+}
+__device__ __forceinline__ void leave_sum(float v, float* part) {
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+}
+template <int T>
+__device__ __forceinline__ float whole_max(const float* part) {
+  float v = part[0];
 #pragma unroll
   for (int i = 1; i < T / 64; ++i) v = fmaxf(v, part[i]);
   return v;
 }
 template <int T>
-__device__ __forceinline__ float group_sum(float v, float* part) {
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = part[0];
+__device__ __forceinline__ float whole_sum(const float* part) {
+  float v = part[0];
 #pragma unroll
   for (int i = 1; i < T / 64; ++i) v += part[i];
   return v;
@@ -103,13 +106,18 @@ struct Teacher {
   double pz;                // sum of p z over the entries on the rows at hand (-inf: one of them is masked)
   float weight;             // weight / tau (NaN: the scores are not numbers)
   int some;                 // there are entries
-  long long id[kMaxK];      // -1: no entry, or not on the rows at hand
-  float p[kMaxK], s[kMaxK]; // probability and logit of such an entry
+  int id[kMaxK];            // the entries' rows (-1: no entry), and their p
+  float p[kMaxK];
+};
+// Entries l and l + 64 of lane l of the wave that makes it.
+struct Entry {
+  int id;         // -1: none, or not on the rows at hand, or listed before
+  float s, all;   // its logit, and all p of its row
 };
 
 // Made by one wave, for rows [i0, i1): lane l has entries l and l + 64.
 template <int DT>
-__device__ __forceinline__ void make_teacher(const DistillArgs& a, long long q, long long i0, long long i1, Teacher& w) {
+__device__ __forceinline__ void make_teacher(const DistillArgs& a, long long q, long long i0, long long i1, Teacher& w, Entry (&mine)[2]) {
   const int lane = threadIdx.x & 63;
   long long id[2];
   float u[2], top = kMinusInf;
@@ -148,10 +156,13 @@ __device__ __forceinline__ void make_teacher(const DistillArgs& a, long long q, 
       const bool here = id[j] >= i0 && id[j] < i1;
       const float s = here ? load_as_f32<DT>(a.logits, q * a.ld + id[j]) : 0.f;
       if (here && p > 0.f) pz += (double)p * ((double)s / (double)a.tau);
-      w.id[lane + 64 * j] = here ? id[j] : -1;
-      w.p[lane + 64 * j] = p;
-      w.s[lane + 64 * j] = s;
+      mine[j] = Entry{here ? (int)id[j] : -1, s, 0.f};
+    } else {
+      mine[j] = Entry{-1, 0.f, 0.f};
     }
+    mine[j].all = p;
+    w.id[lane + 64 * j] = (int)id[j];
+    w.p[lane + 64 * j] = p;
   }
   plogp = wave_sum(plogp);
   pz = wave_sum(pz);
@@ -160,6 +171,30 @@ __device__ __forceinline__ void make_teacher(const DistillArgs& a, long long q, 
     w.pz = pz;
     w.some = some;
     w.weight = mass != mass ? mass : a.weight ? a.weight[q] / a.tau : 0.f;
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's own LDS writes, before it reads them
+  if (!a.grad) return;
+  // Is a row listed twice?  One entry after the other is compared with all lanes' (lists rarely have such
+  // rows, and searches' never: no lane waits for LDS here).
+  const int id0 = (int)id[0], id1 = (int)id[1];
+  bool twice = false;
+  for (int f = 0; f < a.k; ++f) {
+    const int one = __builtin_amdgcn_readlane(f < 64 ? id0 : id1, f & 63);
+    const int n = __popcll(__ballot(id0 == one)) + __popcll(__ballot(id1 == one));
+    twice = twice || (one >= 0 && n > 1);
+  }
+  if (!twice) return;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int own = mine[j].id;
+    float all = 0.f;
+#pragma unroll 1
+    for (int f = 0; f < a.k; ++f)
+      if (w.id[f] == own) {
+        all += w.p[f];
+        if (f < lane + 64 * j) mine[j].id = -1;  // stored once
+      }
+    mine[j].all = all;
   }
 }
 
@@ -216,13 +251,13 @@ __device__ __forceinline__ void load_piece(const void* row, int n, float (&v)[V 
   Vec x[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i)  // past the end: the last vector, not used
-    x[i] = *reinterpret_cast<const Vec*>(p + (unsigned)min(i * T + t, whole - 1) * EV);
+    x[i] = *reinterpret_cast<const Vec*>(static_cast<const char*>(row) + 16u * (unsigned)min(i * T + t, whole - 1));
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int e = 0; e < EV; ++e) {
       const E one = x[i][e];
-      v[i * EV + e] = i * T + t < whole ? load_as_f32<DT>(&one, 0) : kMinusInf;
+      v[i * EV + e] = t < whole - i * T ? load_as_f32<DT>(&one, 0) : kMinusInf;
     }
 }
 
@@ -239,165 +274,226 @@ __device__ __forceinline__ void store_piece(void* row, int n, const float (&v)[V
     Vec x;
 #pragma unroll
     for (int e = 0; e < EV; ++e) x[e] = (E)(some ? v[i * EV + e] * scale : 0.f);
-    if (i * T + t < whole) *reinterpret_cast<Vec*>(p + (unsigned)(i * T + t) * EV) = x;
+    if (t < whole - i * T) *reinterpret_cast<Vec*>(static_cast<char*>(row) + i * (T * 16) + 16u * (unsigned)t) = x;
     __builtin_amdgcn_sched_barrier(0);  // one vector after the other: all products at once would not fit
   }
   if (whole * EV + t < n && t < EV) p[whole * EV + t] = (E)(some ? v[V] * scale : 0.f);
 }
 
-// The entries, once the piece's own stores have arrived: the probability there, less all p of its row (a row that is
-// listed twice is stored once).
+// The entries, once the piece's own stores have arrived: the probability there, less all p of its row.
 template <int DT, typename F>
-__device__ __forceinline__ void store_entries(const DistillArgs& a, long long q, const Teacher& w, F&& prob) {
-  for (int e = threadIdx.x; e < a.k; e += 64) {
-    const long long id = w.id[e];
-    float all = 0.f;
-    bool first = id >= 0;
-    for (int f = 0; f < a.k; ++f)
-      if (w.id[f] == id) {
-        all += w.p[f];
-        first = first && f >= e;
-      }
-    if (first) store_from_f32<DT>(a.grad, q * a.grad_ld + id, w.weight * (prob(w.s[e]) - all));
-  }
+__device__ __forceinline__ void store_entries(const DistillArgs& a, long long q, const Teacher& w, const Entry (&mine)[2],
+                                              F&& prob) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+    if (w.some && mine[j].id >= 0)
+      store_from_f32<DT>(a.grad, q * a.grad_ld + mine[j].id, w.weight * (prob(mine[j].s) - mine[j].all));
 }
 
-// Whole rows of up to T V elements, one workgroup each: the loss, and with GRAD the gradient.
+// Every store of this wave has arrived.
+__device__ __forceinline__ void drain() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+template <int DT>
+__device__ __forceinline__ const char* logits_at(const DistillArgs& a, long long q, long long i) {
+  return static_cast<const char*>(a.logits) + (q * a.ld + i) * size_of<DT>();
+}
+template <int DT>
+__device__ __forceinline__ char* grad_at(const DistillArgs& a, long long q, long long i) {
+  return static_cast<char*>(a.grad) + (q * a.grad_ld + i) * size_of<DT>();
+}
+
+// Whole rows of up to T V elements, one workgroup of T + 64 threads each: the loss, and with GRAD the gradient.
+// (The two sides of the branch meet at the same barriers.)
 template <int DT, int T, int V, bool GRAD>
-__global__ __launch_bounds__(T, 4) void row_kernel(Args p) {
+__global__ __launch_bounds__(T + 64, V == 64 ? 5 : 4) void row_kernel(Args p) {
   const DistillArgs& a = p.a;
   __shared__ float part[2][T / 64];
   __shared__ Teacher w;
-  const int wave = threadIdx.x >> 6;
   const long long q = p.q0 + blockIdx.x;
-  if (wave == 0) make_teacher<DT>(a, q, 0, a.n, w);  // (fp64: before and after the row takes the registers)
-  float v[V + 1];
-  load_piece<DT, T, V>(static_cast<const char*>(a.logits) + q * a.ld * size_of<DT>(), (int)a.n, v);
-  float m = v[0];
-#pragma unroll
-  for (int i = 1; i <= V; ++i) m = fmaxf(m, v[i]);
-  const float s_max = group_max<T>(m, part[0]);
-  const float sum = group_sum<T>(exp_all<V + 1>(v, s_max, p), part[1]);
-  const float unit = inverse(s_max, sum);
-  if constexpr (GRAD) {
-    store_piece<DT, T, V>(static_cast<char*>(a.grad) + q * a.grad_ld * size_of<DT>(), (int)a.n, v, w.some, w.weight * unit);
-    // Every store of the row has arrived before the entries on it are stored again.
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (wave == 0 && w.some)
-      store_entries<DT>(a, q, w, [&](float s1) { return s_max == kMinusInf ? 0.f : exp_diff(s1 - s_max, p) * unit; });
-  }
-  if (threadIdx.x == 0) {
+  if (threadIdx.x >= T) {
+    Entry mine[2];
+    make_teacher<DT>(a, q, 0, a.n, w, mine);
+    lds_barrier();
+    lds_barrier();
+    const float s_max = whole_max<T>(part[0]), sum = whole_sum<T>(part[1]);
     const double lse = lse_of(s_max, sum, a);
-    a.loss[q] = loss_of(w, w.pz, lse);
-    if (a.lse) a.lse[q] = (float)lse;
+    if (threadIdx.x == T) {
+      a.loss[q] = loss_of(w, w.pz, lse);
+      if (a.lse) a.lse[q] = (float)lse;
+    }
+    if constexpr (GRAD) {
+      const float unit = inverse(s_max, sum), s_ref = reference(s_max);
+      lds_barrier();
+      store_entries<DT>(a, q, w, mine, [&](float s) { return exp_diff(s - s_ref, p) * unit; });
+    }
+  } else {
+    float v[V + 1];
+    load_piece<DT, T, V>(logits_at<DT>(a, q, 0), (int)a.n, v);
+    float m = v[0];
+#pragma unroll
+    for (int i = 1; i <= V; ++i) m = fmaxf(m, v[i]);
+    leave_max(m, part[0]);
+    lds_barrier();
+    const float s_max = whole_max<T>(part[0]);
+    leave_sum(exp_all<V + 1>(v, reference(s_max), p), part[1]);
+    lds_barrier();
+    if constexpr (GRAD) {
+      const float unit = inverse(s_max, whole_sum<T>(part[1]));
+      store_piece<DT, T, V>(grad_at<DT>(a, q, 0), (int)a.n, v, w.some, w.weight * unit);
+      drain();
+      lds_barrier();
+    }
   }
 }
 
 // A piece's maximum, sum and sum of p z.
+constexpr int kPieceThreads = 256, kPieceV = kPiece / kPieceThreads;
 template <int DT>
-__global__ __launch_bounds__(256, 4) void piece_kernel(Args p) {
+__global__ __launch_bounds__(kPieceThreads + 64) void piece_kernel(Args p) {
+  constexpr int T = kPieceThreads, V = kPieceV;
   const DistillArgs& a = p.a;
-  __shared__ float part[2][4];
+  __shared__ float part[2][T / 64];
   __shared__ Teacher w;
   const long long q = p.q0 + blockIdx.y, i0 = (long long)blockIdx.x * kPiece, i1 = min(i0 + kPiece, a.n);
-  float v[33];
-  load_piece<DT, 256, 32>(static_cast<const char*>(a.logits) + (q * a.ld + i0) * size_of<DT>(), (int)(i1 - i0), v);
-  if (threadIdx.x < 64) make_teacher<DT>(a, q, i0, i1, w);
-  float m = v[0];
+  if (threadIdx.x >= T) {
+    Entry mine[2];
+    make_teacher<DT>(a, q, i0, i1, w, mine);
+    lds_barrier();
+    lds_barrier();
+    if (threadIdx.x == T)
+      p.pieces[q * p.n_pieces + blockIdx.x] = Piece{whole_max<T>(part[0]), whole_sum<T>(part[1]), w.pz};
+  } else {
+    float v[V + 1];
+    load_piece<DT, T, V>(logits_at<DT>(a, q, i0), (int)(i1 - i0), v);
+    float m = v[0];
 #pragma unroll
-  for (int i = 1; i <= 32; ++i) m = fmaxf(m, v[i]);
-  const float s_max = group_max<256>(m, part[0]);
-  const float sum = group_sum<256>(exp_all<33>(v, s_max, p), part[1]);
-  if (threadIdx.x == 0) p.pieces[q * p.n_pieces + blockIdx.x] = Piece{s_max, sum, w.pz};
+    for (int i = 1; i <= V; ++i) m = fmaxf(m, v[i]);
+    leave_max(m, part[0]);
+    lds_barrier();
+    leave_sum(exp_all<V + 1>(v, reference(whole_max<T>(part[0])), p), part[1]);
+    lds_barrier();
+  }
 }
 
-// A query's pieces as one, in every thread of a workgroup of 256.
-__device__ __forceinline__ Piece join(const Args& p, long long q, float* part, double* part64) {
+// A query's pieces as one: two halves with a barrier between and one after, by 256 threads.
+struct Join {
+  float max[4];
+  double sum[4], pz[4];
+};
+__device__ __forceinline__ void join_max(const Args& p, long long q, Join& j) {
   const Piece* from = p.pieces + q * p.n_pieces;
   float m = kMinusInf;
   for (int i = threadIdx.x; i < p.n_pieces; i += 256) m = fmaxf(m, from[i].max);
-  m = group_max<256>(m, part);
+  leave_max(m, j.max);
+}
+__device__ __forceinline__ void join_sum(const Args& p, long long q, Join& j) {
+  const Piece* from = p.pieces + q * p.n_pieces;
+  const float ref = reference(whole_max<256>(j.max));
   double sum = 0.0, pz = 0.0;
   for (int i = threadIdx.x; i < p.n_pieces; i += 256) {
     const Piece x = from[i];
-    sum += (double)x.sum * (m == kMinusInf ? 1.0 : (double)exp_diff(x.max - m, p));
+    sum += x.max == kMinusInf ? (double)x.sum : (double)x.sum * (double)exp_diff(x.max - ref, p);  // (its sum: 0 or NaN)
     pz += x.pz;
   }
   sum = wave_sum(sum);
   pz = wave_sum(pz);
   if ((threadIdx.x & 63) == 0) {
-    part64[threadIdx.x >> 6] = sum;
-    part64[4 + (threadIdx.x >> 6)] = pz;
+    j.sum[threadIdx.x >> 6] = sum;
+    j.pz[threadIdx.x >> 6] = pz;
   }
-  __syncthreads();
-  return Piece{m, (float)(part64[0] + part64[1] + part64[2] + part64[3]), part64[4] + part64[5] + part64[6] + part64[7]};
+}
+__device__ __forceinline__ Piece joined(const Join& j) {
+  return Piece{whole_max<256>(j.max), (float)(j.sum[0] + j.sum[1] + j.sum[2] + j.sum[3]), j.pz[0] + j.pz[1] + j.pz[2] + j.pz[3]};
 }
 
 // Whole queries from their pieces: loss and lse, and what the gradient of very long rows needs.
 template <int DT>
-__global__ __launch_bounds__(256) void join_kernel(Args p) {
-  __shared__ float part[4];
-  __shared__ double part64[8];
-  __shared__ Teacher w;
+__global__ __launch_bounds__(256 + 64) void join_kernel(Args p) {
   const DistillArgs& a = p.a;
+  __shared__ Join j;
+  __shared__ Teacher w;
   const long long q = p.q0 + blockIdx.x;
-  if (threadIdx.x < 64) make_teacher<DT>(a, q, 0, 0, w);
-  const Piece x = join(p, q, part, part64);
-  if (threadIdx.x == 0) {
-    const double lse = lse_of(x.max, x.sum, a);
-    a.loss[q] = loss_of(w, x.pz, lse);
-    if (a.lse) a.lse[q] = (float)lse;
-    if (p.joined) p.joined[q] = x;
+  if (threadIdx.x >= 256) {
+    Entry mine[2];
+    make_teacher<DT>(a, q, 0, 0, w, mine);
+    lds_barrier();
+    lds_barrier();
+    if (threadIdx.x == 256) {
+      const Piece x = joined(j);
+      const double lse = lse_of(x.max, x.sum, a);
+      a.loss[q] = loss_of(w, x.pz, lse);
+      if (a.lse) a.lse[q] = (float)lse;
+      if (p.joined) p.joined[q] = x;
+    }
+  } else {
+    join_max(p, q, j);
+    lds_barrier();
+    join_sum(p, q, j);
+    lds_barrier();
   }
 }
 
 // The gradient of a piece: from lse (LSE), or from the query's pieces, with the loss by its first workgroup.
 template <int DT, bool LSE>
-__global__ __launch_bounds__(256, 4) void grad_kernel(Args p) {
+__global__ __launch_bounds__(kPieceThreads + 64) void grad_kernel(Args p) {
+  constexpr int T = kPieceThreads, V = kPieceV;
+  static_assert(T == 256, "the join's threads");
   const DistillArgs& a = p.a;
-  __shared__ float part[4];
-  __shared__ double part64[8];
+  __shared__ Join j;
   __shared__ Teacher w;
   const long long q = p.q0 + blockIdx.y, i0 = (long long)blockIdx.x * kPiece, i1 = min(i0 + kPiece, a.n);
-  float v[33];
-  load_piece<DT, 256, 32>(static_cast<const char*>(a.logits) + (q * a.ld + i0) * size_of<DT>(), (int)(i1 - i0), v);
-  if (threadIdx.x < 64) make_teacher<DT>(a, q, i0, i1, w);
-  Piece x{};
-  float l_hi = 0.f, l_lo = 0.f, unit = 1.f;
-  if constexpr (LSE) {
-    // lse log2(e) in two parts; z_i - lse is formed from the exact product s c.
-    const double l = (double)a.lse_in[q] * 1.4426950408889634074;
-    l_hi = (float)l;
-    l_lo = fabsf(l_hi) < __builtin_inff() ? (float)(l - (double)l_hi) : 0.f;
-    __syncthreads();
-  } else {
-    if (p.joined) {
-      x = p.joined[q];
-      __syncthreads();
+  // Past the barriers: what a probability is made from.
+  float l_hi = 0.f, l_lo = 0.f, s_ref = 0.f, unit = 1.f;
+  auto set = [&] {
+    if constexpr (LSE) {
+      // lse log2(e) in two parts; z_i - lse is formed from the exact product s c.
+      const double l = (double)a.lse_in[q] * 1.4426950408889634074;
+      l_hi = (float)l;
+      l_lo = fabsf(l_hi) < __builtin_inff() ? (float)(l - (double)l_hi) : 0.f;
     } else {
-      x = join(p, q, part, part64);
-      if (threadIdx.x == 0 && i0 == 0) a.loss[q] = loss_of(w, x.pz, lse_of(x.max, x.sum, a));
+      const Piece x = p.joined ? p.joined[q] : joined(j);
+      s_ref = reference(x.max);
+      unit = inverse(x.max, x.sum);
+      return x;
     }
-    unit = inverse(x.max, x.sum);
-  }
-  const float x_max = x.max == kMinusInf ? 0.f : x.max;
+  };
   auto prob = [&](float s) {
     if constexpr (LSE) {
       const float hi = s * p.c_hi, lo = fmaf(s, p.c_hi, -hi) + s * p.c_lo;
       return hi == kMinusInf ? (l_hi != l_hi ? l_hi : 0.f) : __builtin_amdgcn_exp2f((hi - l_hi) + (lo - l_lo));
     } else {
-      return exp_diff(s - x_max, p);  // (every logit -inf: 0 and unit 0)
+      return exp_diff(s - s_ref, p);
     }
   };
+  if (threadIdx.x >= T) {
+    Entry mine[2];
+    make_teacher<DT>(a, q, i0, i1, w, mine);
+    lds_barrier();
+    if constexpr (!LSE) lds_barrier();
+    if constexpr (LSE) {
+      set();
+    } else {
+      const Piece x = set();
+      if (!p.joined && i0 == 0 && threadIdx.x == T) a.loss[q] = loss_of(w, x.pz, lse_of(x.max, x.sum, a));
+    }
+    lds_barrier();
+    store_entries<DT>(a, q, w, mine, [&](float s) { return prob(s) * unit; });
+  } else {
+    float v[V + 1];
+    load_piece<DT, T, V>(logits_at<DT>(a, q, i0), (int)(i1 - i0), v);
+    if constexpr (!LSE) {
+      if (!p.joined) join_max(p, q, j);
+      lds_barrier();
+      if (!p.joined) join_sum(p, q, j);
+    }
+    lds_barrier();
+    set();
 #pragma unroll
-  for (int i = 0; i <= 32; ++i) v[i] = prob(v[i]);
-  store_piece<DT, 256, 32>(static_cast<char*>(a.grad) + (q * a.grad_ld + i0) * size_of<DT>(), (int)(i1 - i0), v, w.some,
-                           w.weight * unit);
-  // Every store of the piece has arrived before the entries on it are stored again.
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (threadIdx.x < 64 && w.some) store_entries<DT>(a, q, w, [&](float s1) { return prob(s1) * unit; });
+    for (int i = 0; i <= V; ++i) v[i] = prob(v[i]);
+    store_piece<DT, T, V>(grad_at<DT>(a, q, i0), (int)(i1 - i0), v, w.some, w.weight * unit);
+    drain();
+    lds_barrier();
+  }
 }
 
 int pieces_of(long long n) { return (int)((n + kPiece - 1) / kPiece); }
@@ -425,15 +521,15 @@ hipError_t launch_distill(const DistillArgs& a, void* ws, hipStream_t s) {
       const unsigned nq = (unsigned)std::min(kSlab, a.nq - p.q0);
       const dim3 grid((unsigned)p.n_pieces, nq);
       if (!a.loss) {
-        grad_kernel<dt(), true><<<grid, 256, 0, s>>>(p);
+        grad_kernel<dt(), true><<<grid, kPieceThreads + 64, 0, s>>>(p);
       } else if (a.n <= kRow) {
         auto rows = [&](auto grad) {
           if (a.n <= 256 * 16)
-            row_kernel<dt(), 256, 16, grad()><<<nq, 256, 0, s>>>(p);
+            row_kernel<dt(), 256, 16, grad()><<<nq, 256 + 64, 0, s>>>(p);
           else if (a.n <= 512 * 32)
-            row_kernel<dt(), 512, 32, grad()><<<nq, 512, 0, s>>>(p);
+            row_kernel<dt(), 512, 32, grad()><<<nq, 512 + 64, 0, s>>>(p);
           else
-            row_kernel<dt(), 512, 64, grad()><<<nq, 512, 0, s>>>(p);
+            row_kernel<dt(), 512, 64, grad()><<<nq, 512 + 64, 0, s>>>(p);
         };
         if (a.grad)
           rows(std::true_type{});
@@ -441,9 +537,9 @@ hipError_t launch_distill(const DistillArgs& a, void* ws, hipStream_t s) {
           rows(std::false_type{});
       } else {
         p.joined = a.grad && p.n_pieces > kJoinHere ? p.pieces + a.nq * p.n_pieces : nullptr;
-        piece_kernel<dt()><<<grid, 256, 0, s>>>(p);
-        if (!a.grad || p.joined) join_kernel<dt()><<<nq, 256, 0, s>>>(p);
-        if (a.grad) grad_kernel<dt(), false><<<grid, 256, 0, s>>>(p);
+        piece_kernel<dt()><<<grid, kPieceThreads + 64, 0, s>>>(p);
+        if (!a.grad || p.joined) join_kernel<dt()><<<nq, 256 + 64, 0, s>>>(p);
+        if (a.grad) grad_kernel<dt(), false><<<grid, kPieceThreads + 64, 0, s>>>(p);
       }
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
