@@ -100,112 +100,117 @@ __device__ __forceinline__ X wave_sum(X v) {
   return v;
 }
 
-// A query's teacher, in LDS.
+// What the other waves need of a query's teacher.
 struct Teacher {
-  double plogp;             // sum of p log p
-  double pz;                // sum of p z over the entries on the rows at hand (-inf: one of them is masked)
-  float weight;             // weight / tau (NaN: the scores are not numbers)
-  int some;                 // there are entries
-  int id[kMaxK];            // the entries' rows (-1: no entry), and their p
-  float p[kMaxK];
+  float weight;  // weight / tau (NaN: the scores are not numbers)
+  int some;      // there are entries
 };
-// Entries l and l + 64 of lane l of the wave that makes it.
-struct Entry {
-  int id;         // -1: none, or not on the rows at hand, or listed before
-  float s, all;   // its logit, and all p of its row
+// A set of rows of a piece.
+template <int ROWS>
+struct RowSet {
+  unsigned bits[ROWS / 32];
 };
 
-// Made by one wave, for rows [i0, i1): lane l has entries l and l + 64.
-template <int DT>
-__device__ __forceinline__ void make_teacher(const DistillArgs& a, long long q, long long i0, long long i1, Teacher& w, Entry (&mine)[2]) {
-  const int lane = threadIdx.x & 63;
-  long long id[2];
-  float u[2], top = kMinusInf;
-  int some = 0;
+// A query's teacher for rows [i0, i1), made by one wave: lane l has entries l and l + 64.
+struct Entries {
+  int id[2];      // -1: none
+  float u[2], p[2];
+  float s[2];     // logit, of an entry on the rows at hand
+  float all[2];   // all p of its row
+  bool own[2];    // on the rows at hand, and not listed before
+  float top, mass;
+  double plogp, pz;  // sums of p log p, and of p z over the rows at hand (-inf: an entry on a masked row)
+
+  // What the others wait for.
+  template <int DT>
+  __device__ __forceinline__ void begin(const DistillArgs& a, long long q, long long i0, long long i1, Teacher& w) {
+    const int lane = threadIdx.x & 63;
+    long long at[2];
+    float t[2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int e = lane + 64 * j;
-    id[j] = -1;
-    u[j] = kMinusInf;
-    if (e < a.k) {
-      const long long at = a.ids[q * a.k + e];
-      const float t = a.t[q * a.k + e];
-      if (at >= 0 && at < a.n && t > kMinusInf) {
-        id[j] = at;
-        u[j] = t / a.t_tau;
-        some = 1;  // (one whose quotient is -inf has p = 0, but is an entry)
-      }
+    for (int j = 0; j < 2; ++j) {
+      const long long e = q * a.k + min(lane + 64 * j, a.k - 1);
+      at[j] = a.ids[e];
+      t[j] = a.t[e];
     }
-    top = fmaxf(top, u[j]);
-  }
-  for (int o = 32; o > 0; o >>= 1) {
-    top = fmaxf(top, __shfl_xor(top, o));
-    some |= __shfl_xor(some, o);
-  }
-  float x[2];
+    const float weight = a.weight ? a.weight[q] : 0.f;
+    top = kMinusInf;
 #pragma unroll
-  for (int j = 0; j < 2; ++j)  // (all quotients -inf: the entries are equal; an infinite one: NaN)
-    x[j] = id[j] < 0 ? 0.f : u[j] == top ? (top == kMinusInf ? 1.f : top - top + 1.f) : expf(u[j] - top);
-  const float mass = wave_sum(x[0] + x[1]);
-  double plogp = 0.0, pz = 0.0;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const float p = id[j] < 0 ? 0.f : x[j] / mass;
-    if (p > 0.f) plogp += (double)p * ((u[j] == top ? 0.0 : (double)(u[j] - top)) - log((double)mass));
-    if (lane + 64 * j < a.k) {
-      const bool here = id[j] >= i0 && id[j] < i1;
-      const float s = here ? load_as_f32<DT>(a.logits, q * a.ld + id[j]) : 0.f;
-      if (here && p > 0.f) pz += (double)p * ((double)s / (double)a.tau);
-      mine[j] = Entry{here ? (int)id[j] : -1, s, 0.f};
-    } else {
-      mine[j] = Entry{-1, 0.f, 0.f};
+    for (int j = 0; j < 2; ++j) {
+      const bool entry = lane + 64 * j < a.k && at[j] >= 0 && at[j] < a.n && t[j] > kMinusInf;
+      id[j] = entry ? (int)at[j] : -1;
+      own[j] = id[j] >= i0 && id[j] < i1;
+      s[j] = 0.f;
+      if (own[j]) s[j] = load_as_f32<DT>(a.logits, q * a.ld + id[j]);
+      u[j] = entry ? t[j] / a.t_tau : kMinusInf;
+      top = fmaxf(top, u[j]);
     }
-    mine[j].all = p;
-    w.id[lane + 64 * j] = (int)id[j];
-    w.p[lane + 64 * j] = p;
-  }
-  plogp = wave_sum(plogp);
-  pz = wave_sum(pz);
-  if (lane == 0) {
-    w.plogp = plogp;
-    w.pz = pz;
-    w.some = some;
-    w.weight = mass != mass ? mass : a.weight ? a.weight[q] / a.tau : 0.f;
-  }
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's own LDS writes, before it reads them
-  if (!a.grad) return;
-  // Is a row listed twice?  One entry after the other is compared with all lanes' (lists rarely have such
-  // rows, and searches' never: no lane waits for LDS here).
-  const int id0 = (int)id[0], id1 = (int)id[1];
-  bool twice = false;
-  for (int f = 0; f < a.k; ++f) {
-    const int one = __builtin_amdgcn_readlane(f < 64 ? id0 : id1, f & 63);
-    const int n = __popcll(__ballot(id0 == one)) + __popcll(__ballot(id1 == one));
-    twice = twice || (one >= 0 && n > 1);
-  }
-  if (!twice) return;
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int own = mine[j].id;
-    float all = 0.f;
-#pragma unroll 1
-    for (int f = 0; f < a.k; ++f)
-      if (w.id[f] == own) {
-        all += w.p[f];
-        if (f < lane + 64 * j) mine[j].id = -1;  // stored once
-      }
-    mine[j].all = all;
+    for (int j = 0; j < 2; ++j)  // (an entry whose quotient is -inf is one all the same; an infinite quotient: NaN)
+      p[j] = id[j] < 0 ? 0.f : u[j] == top ? (top == kMinusInf ? 1.f : top - top + 1.f) : expf(u[j] - top);
+    mass = wave_sum(p[0] + p[1]);
+    const bool some = __ballot(id[0] >= 0 || id[1] >= 0) != 0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) p[j] = id[j] < 0 ? 0.f : p[j] / mass;
+    if (lane == 0) w = Teacher{mass != mass ? mass : weight / a.tau, some};
   }
+
+  // The sums, and the rows that are listed twice: they are stored once.  `set`: see clear().  (Searches never
+  // list a row twice; one look at a set of bits tells whether a list does.)
+  template <int ROWS>
+  __device__ __forceinline__ void finish(const DistillArgs& a, long long i0, RowSet<ROWS>& set) {
+    const int lane = threadIdx.x & 63;
+    plogp = pz = 0.0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (p[j] > 0.f) {
+        if (u[j] != top) plogp += (double)p[j] * (double)(u[j] - top);
+        if (own[j]) pz += (double)p[j] * ((double)s[j] / (double)a.tau);
+      }
+      all[j] = p[j];
+    }
+    plogp = wave_sum(plogp) - log((double)mass);
+    pz = wave_sum(pz);
+    if (!a.grad) return;
+    bool twice = false;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (own[j]) {
+        const unsigned at = (unsigned)(id[j] - i0), bit = 1u << (at & 31);
+        twice = twice || (atomicOr(&set.bits[at / 32], bit) & bit);
+      }
+    if (__ballot(twice) == 0) return;
+    float sum[2] = {0.f, 0.f};
+    for (int f = 0; f < a.k; ++f) {
+      const int one = __builtin_amdgcn_readlane(f < 64 ? id[0] : id[1], f & 63);
+      const float p1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f < 64 ? p[0] : p[1]), f & 63));
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (id[j] == one) {
+          sum[j] += p1;
+          if (f < lane + 64 * j) own[j] = false;
+        }
+    }
+    all[0] = sum[0];
+    all[1] = sum[1];
+  }
+};
+
+// Empties the set, by the wave that will use it.
+template <int ROWS>
+__device__ __forceinline__ void clear(RowSet<ROWS>& set) {
+  for (int i = threadIdx.x & 63; i < ROWS / 128; i += 64) reinterpret_cast<uint4*>(set.bits)[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
 __device__ __forceinline__ double lse_of(float s_max, float sum, const DistillArgs& a) {
   return s_max == kMinusInf && sum == sum ? -__builtin_inf() : (double)s_max / (double)a.tau + log((double)sum);
 }
-__device__ __forceinline__ float loss_of(const Teacher& w, double pz, double lse) {
-  if (!w.some) return 0.f;
-  if (w.weight != w.weight || lse != lse || pz != pz) return __builtin_nanf("");
+__device__ __forceinline__ float loss_of(const Entries& e, bool some, double pz, double lse) {
+  if (!some) return 0.f;
+  if (e.mass != e.mass || lse != lse || pz != pz) return __builtin_nanf("");
   if (pz == -__builtin_inf()) return __builtin_inff();
-  return (float)(w.plogp - pz + lse);
+  return (float)(e.plogp - pz + lse);
 }
 
 // The elements of a piece that thread t of T holds: V in 16-byte vectors, vector i at (i T + t) EV, and of what is left
@@ -282,12 +287,10 @@ __device__ __forceinline__ void store_piece(void* row, int n, const float (&v)[V
 
 // The entries, once the piece's own stores have arrived: the probability there, less all p of its row.
 template <int DT, typename F>
-__device__ __forceinline__ void store_entries(const DistillArgs& a, long long q, const Teacher& w, const Entry (&mine)[2],
-                                              F&& prob) {
+__device__ __forceinline__ void store_entries(const DistillArgs& a, long long q, const Teacher& w, const Entries& e, F&& prob) {
 #pragma unroll
   for (int j = 0; j < 2; ++j)
-    if (w.some && mine[j].id >= 0)
-      store_from_f32<DT>(a.grad, q * a.grad_ld + mine[j].id, w.weight * (prob(mine[j].s) - mine[j].all));
+    if (e.own[j]) store_from_f32<DT>(a.grad, q * a.grad_ld + e.id[j], w.weight * (prob(e.s[j]) - e.all[j]));
 }
 
 // Every store of this wave has arrived.
@@ -309,22 +312,25 @@ __global__ __launch_bounds__(T + 64, V == 64 ? 5 : 4) void row_kernel(Args p) {
   const DistillArgs& a = p.a;
   __shared__ float part[2][T / 64];
   __shared__ Teacher w;
+  __shared__ __attribute__((aligned(16))) RowSet<GRAD ? T * V : 128> set;
   const long long q = p.q0 + blockIdx.x;
   if (threadIdx.x >= T) {
-    Entry mine[2];
-    make_teacher<DT>(a, q, 0, a.n, w, mine);
+    Entries e;
+    if (GRAD) clear(set);
+    e.begin<DT>(a, q, 0, a.n, w);
     lds_barrier();
+    e.finish(a, 0, set);
     lds_barrier();
     const float s_max = whole_max<T>(part[0]), sum = whole_sum<T>(part[1]);
     const double lse = lse_of(s_max, sum, a);
     if (threadIdx.x == T) {
-      a.loss[q] = loss_of(w, w.pz, lse);
+      a.loss[q] = loss_of(e, w.some, e.pz, lse);
       if (a.lse) a.lse[q] = (float)lse;
     }
     if constexpr (GRAD) {
       const float unit = inverse(s_max, sum), s_ref = reference(s_max);
       lds_barrier();
-      store_entries<DT>(a, q, w, mine, [&](float s) { return exp_diff(s - s_ref, p) * unit; });
+      store_entries<DT>(a, q, w, e, [&](float s) { return exp_diff(s - s_ref, p) * unit; });
     }
   } else {
     float v[V + 1];
@@ -354,14 +360,17 @@ __global__ __launch_bounds__(kPieceThreads + 64) void piece_kernel(Args p) {
   const DistillArgs& a = p.a;
   __shared__ float part[2][T / 64];
   __shared__ Teacher w;
+  __shared__ __attribute__((aligned(16))) RowSet<kPiece> set;
   const long long q = p.q0 + blockIdx.y, i0 = (long long)blockIdx.x * kPiece, i1 = min(i0 + kPiece, a.n);
   if (threadIdx.x >= T) {
-    Entry mine[2];
-    make_teacher<DT>(a, q, i0, i1, w, mine);
+    Entries e;
+    clear(set);
+    e.begin<DT>(a, q, i0, i1, w);
     lds_barrier();
+    e.finish(a, i0, set);
     lds_barrier();
     if (threadIdx.x == T)
-      p.pieces[q * p.n_pieces + blockIdx.x] = Piece{whole_max<T>(part[0]), whole_sum<T>(part[1]), w.pz};
+      p.pieces[q * p.n_pieces + blockIdx.x] = Piece{whole_max<T>(part[0]), whole_sum<T>(part[1]), e.pz};
   } else {
     float v[V + 1];
     load_piece<DT, T, V>(logits_at<DT>(a, q, i0), (int)(i1 - i0), v);
@@ -412,16 +421,19 @@ __global__ __launch_bounds__(256 + 64) void join_kernel(Args p) {
   const DistillArgs& a = p.a;
   __shared__ Join j;
   __shared__ Teacher w;
+  __shared__ __attribute__((aligned(16))) RowSet<128> set;
   const long long q = p.q0 + blockIdx.x;
   if (threadIdx.x >= 256) {
-    Entry mine[2];
-    make_teacher<DT>(a, q, 0, 0, w, mine);
+    Entries e;
+    clear(set);
+    e.begin<DT>(a, q, 0, 0, w);
     lds_barrier();
+    e.finish(a, 0, set);
     lds_barrier();
     if (threadIdx.x == 256) {
       const Piece x = joined(j);
       const double lse = lse_of(x.max, x.sum, a);
-      a.loss[q] = loss_of(w, x.pz, lse);
+      a.loss[q] = loss_of(e, w.some, x.pz, lse);
       if (a.lse) a.lse[q] = (float)lse;
       if (p.joined) p.joined[q] = x;
     }
@@ -441,6 +453,7 @@ __global__ __launch_bounds__(kPieceThreads + 64) void grad_kernel(Args p) {
   const DistillArgs& a = p.a;
   __shared__ Join j;
   __shared__ Teacher w;
+  __shared__ __attribute__((aligned(16))) RowSet<kPiece> rows;
   const long long q = p.q0 + blockIdx.y, i0 = (long long)blockIdx.x * kPiece, i1 = min(i0 + kPiece, a.n);
   // Past the barriers: what a probability is made from.
   float l_hi = 0.f, l_lo = 0.f, s_ref = 0.f, unit = 1.f;
@@ -466,18 +479,21 @@ __global__ __launch_bounds__(kPieceThreads + 64) void grad_kernel(Args p) {
     }
   };
   if (threadIdx.x >= T) {
-    Entry mine[2];
-    make_teacher<DT>(a, q, i0, i1, w, mine);
+    Entries e;
+    clear(rows);
+    e.begin<DT>(a, q, i0, i1, w);
+    if (LSE && a.grad == a.logits) drain();  // the entries' logits, before the others store over them
     lds_barrier();
-    if constexpr (!LSE) lds_barrier();
+    e.finish(a, i0, rows);
     if constexpr (LSE) {
       set();
     } else {
+      lds_barrier();
       const Piece x = set();
-      if (!p.joined && i0 == 0 && threadIdx.x == T) a.loss[q] = loss_of(w, x.pz, lse_of(x.max, x.sum, a));
+      if (!p.joined && i0 == 0 && threadIdx.x == T) a.loss[q] = loss_of(e, w.some, x.pz, lse_of(x.max, x.sum, a));
     }
     lds_barrier();
-    store_entries<DT>(a, q, w, mine, [&](float s) { return prob(s) * unit; });
+    store_entries<DT>(a, q, w, e, [&](float s) { return prob(s) * unit; });
   } else {
     float v[V + 1];
     load_piece<DT, T, V>(logits_at<DT>(a, q, i0), (int)(i1 - i0), v);
