@@ -25,21 +25,6 @@ __device__ __forceinline__ float mx_decode(unsigned code) {
   return (code & kSign) ? -mag : mag;
 }
 
-// Code of y, |y| < 8 (larger and infinite ones saturate): y is rounded to the nearest multiple, ties to
-// even, of the step of its binade by adding 1.5 x 2^23 steps, whose low bits then count them.
-template <int BITS>
-__device__ __forceinline__ unsigned mx_encode(float y) {
-  constexpr unsigned kSign = 1u << (BITS - 1);
-  constexpr unsigned kHalf = 1u << (BITS - 3);     // codes per binade
-  constexpr int kStep = BITS == 4 ? -1 : -3;       // log2 of the step below 2
-  const float a = fabsf(y);
-  const int ex = min(max((int)(__float_as_uint(a) >> 23) - 127, 0), 2);
-  const float magic = __uint_as_float((unsigned)(127 + 23 + kStep + ex) << 23 | 0x400000u);
-  const unsigned steps = __float_as_uint(fminf(a, 8.f) + magic) & 0xffu;
-  const unsigned code = min(steps + kHalf * (unsigned)ex, kSign - 1);
-  return code | (__float_as_uint(y) >> 31) * kSign;
-}
-
 template <int DT>
 __device__ __forceinline__ float load_as_f32(const void* p, long long i) {
   if constexpr (DT == kDtypeF32) {
