@@ -4,17 +4,27 @@
 // and 16 queries over 128 elements (four blocks: a step), in 4 or 6 bits, and applies both scale
 // bytes of every block itself; its sums are fp32.  A lane l holds block l / 16 of row l % 16.
 //
-// A workgroup keeps a block of QT x 16 queries in LDS and passes over a run of row tiles.  A wave
-// owns RT x 16 rows of a tile and loads them straight into registers (no other wave needs them),
-// a set of four steps ahead of the products.  Four neighbouring lanes load 64 (96) contiguous bytes of one
-// row, then of the next, and exchange them: lane by lane as the instruction wants its
-// operands, every load would touch 64 cache lines.  (Measured so: 2 TB/s of rows at best.)
+// A workgroup keeps a block of QT x 16 queries in LDS and passes over a run of row tiles.  A wave owns RT x 16 rows
+// of a tile (with WQ > 1, WQ waves own the same rows, each with its part of the queries) and loads them straight
+// into registers, a set of four steps ahead of the products.  Four neighbouring lanes load 64 (96)
+// contiguous bytes of one row, then of the next, and exchange them: lane by lane as the instruction
+// wants its operands, every load would touch 64 cache lines.  (Measured so: 2 TB/s of rows at best.)
 // Which blocks of a set make a step is free, as long as both sides agree: lane group a = l / 16
 // has blocks 4 a .. 4 a + 3, one per step, so its four scale bytes are one dword.  Of a last set of
 // s < 4 steps it has blocks s a .. s a + s - 1.
 //
 // The sums pass by the caches (nontemporal): kept there, they push out the rows that the other
-// query blocks of the chunk are about to read (1,024 x 262,144 fp32: 430 us, 270 without them).
+// query blocks of the chunk are about to read (1,024 x 262,144 x 768, 6 and 4 bits, to fp32: 337 us, 287 without
+// them).  They are stored in whole lines of 128 bytes, two subtiles of fp32 together or, in 16 bits, two
+// parts of a tile (PAIR; the first waits in registers): stores of half lines alone take 185 us for 537 MB,
+// of whole ones 119.
+//
+// Measured, rows and sums read and written once: 1,024 x 262,144 x 768 (6 and 4 bits) to bf16 256 us, 2.5 TB/s, 1.6
+// PFLOP/s; to fp32 287 us, 4.1 TB/s; 128 x 2,000,000 x 768 to bf16 286 us, 4.6 TB/s; 256 x 32,768 x 1,024 to
+// fp32 17 us, 3.0 TB/s; 1,024 x 32,768 x 4,096 (queries do not fit LDS) to bf16 214 us, 1.3 PFLOP/s.
+// Without its stores the first takes 187 us, without its loads 228: bound by the memory's latency under stores, of
+// which two sets in flight hide a part, and by LDS, from which every product reads its queries.  Three or
+// four subtiles of rows a wave, or sets further ahead, take more registers than there are.
 #include <algorithm>
 
 #include "mfma.h"
@@ -34,6 +44,7 @@ struct ScoresArgs {
   int dtype;
   int n_qblocks, n_chunks;
   int least, spare;  // row tiles of a chunk; the first `spare` chunks have one more
+  int turn;          // the query blocks of a chunk begin each `turn` of its tiles with another one
 };
 
 template <int RB, int QB, int STEP>
@@ -57,13 +68,6 @@ __device__ __forceinline__ void load_block(unsigned (&w)[BITS], const unsigned c
   }
 }
 
-// The four bytes from p + at on.  Reads none past p + bytes (at least 4): those come back as what they are not.
-__device__ __forceinline__ unsigned load_scales(const unsigned char* p, unsigned at, unsigned bytes) {
-  const unsigned from = min(at, bytes - 4);
-  unsigned v;
-  __builtin_memcpy(&v, p + from, 4);
-  return v >> (8 * min(at - from, 3u));
-}
 // The n bytes (1 to 4) from p on, by the aligned words that hold the first and the last of them.
 __device__ __forceinline__ unsigned load_bytes(const unsigned char* p, int n) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p);
@@ -101,6 +105,27 @@ __device__ __forceinline__ void transpose4(unsigned (&w)[4][RB], bool odd, bool 
   }
 }
 
+// `keep`, and in the lanes whose group of four within sixteen MASK names `take` of the lane eight away.
+template <int MASK>
+__device__ __forceinline__ unsigned swap_eight(unsigned keep, unsigned take) {
+  return (unsigned)__builtin_amdgcn_update_dpp((int)keep, (int)take, 0x128, 0xf, MASK, false);
+}
+
+// Two sums in a 16-bit type.
+__device__ __forceinline__ unsigned pack16(int dtype, float a, float b) {
+  typedef __bf16 B2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 H2 __attribute__((ext_vector_type(2)));
+  const B2 x = {(__bf16)a, (__bf16)b};
+  const H2 y = {(_Float16)a, (_Float16)b};
+  return dtype == kDtypeBF16 ? __builtin_bit_cast(unsigned, x) : __builtin_bit_cast(unsigned, y);
+}
+// Sixteen bytes at a 16-bit element's address.
+__device__ __forceinline__ void store_line(unsigned short* p, const unsigned (&v)[4]) {
+  typedef unsigned V __attribute__((ext_vector_type(4), aligned(2)));
+  const V o = {v[0], v[1], v[2], v[3]};
+  __builtin_nontemporal_store(o, reinterpret_cast<V*>(p));
+}
+
 // Sets (512 elements) of the queries that LDS holds.
 template <int QT>
 constexpr int lds_sets() {
@@ -123,12 +148,13 @@ __device__ __forceinline__ void store_rows(T* p, const float (&v)[N], long long 
   }
 }
 
-// W waves, each with RT x 16 rows of a tile.  TAIL: the rows fill no tile.  Otherwise the last tile ends with the last
+// W waves, WQ to the same rows, each with RT x 16 rows of a part of a tile.  PAIR: tiles of two parts, a wave's rows
+// of both next to each other.  TAIL: the rows fill no tile.  Otherwise the last tile ends with the last
 // row, and computes some rows that the tile before it has too, to the same bits.
 // RES: LDS holds all sets of the queries.
-template <int QB, int RB, int W, int RT, int QT, bool RES, bool TAIL>
+template <int QB, int RB, int W, int WQ, int RT, int QT, bool RES, bool PAIR, bool TAIL>
 __global__ __launch_bounds__(W * 64, 2) void scores_kernel(ScoresArgs p) {
-  constexpr int KC = lds_sets<QT>(), ROWS = W * RT * 16;
+  constexpr int KC = lds_sets<QT>(), PARTS = PAIR ? 2 : 1, ROWS = W / WQ * PARTS * RT * 16, QW = QT / WQ;
   // [kc][QT][16 queries][16 blocks] codes, block c of query q at c ^ q: their first 16 bytes, and the
   // other 8; [kc][QT][64 lanes] scale bytes of a lane's four steps
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -138,6 +164,7 @@ __global__ __launch_bounds__(W * 64, 2) void scores_kernel(ScoresArgs p) {
   uint2* lds_hi = reinterpret_cast<uint2*>(lds_lo + kc * QT * 256);
   unsigned* lds_s = reinterpret_cast<unsigned*>(lds + kc * QT * 256 * (4 * QB));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wave / WQ, wq = wave % WQ * QW;  // a wave's rows and its first query tile
   const int r16 = lane & 15, g = lane >> 4, b4 = (lane >> 2) & 3, c4 = lane & 3;
   const unsigned row_bytes = (unsigned)nb * (4 * RB);
   // A lane's stores are of 16 bytes: 4 consecutive rows in fp32, 8 in 16 bits (4 where it has only those).
@@ -153,6 +180,9 @@ __global__ __launch_bounds__(W * 64, 2) void scores_kernel(ScoresArgs p) {
     // Sets [first, first + KC) of the queries to LDS.  Past a row's last block both sides take some block's codes
     // (finite, as any codes are) under the smallest scale: 2^-254 times such products are zero in fp32.
     auto stage = [&](int first) {
+      int lane = threadIdx.x & 63;
+      if constexpr (RES) asm volatile("" : "+v"(lane));  // (its addresses are not to be kept in registers over the tiles)
+      const int r16 = lane & 15, g = lane >> 4, b4 = (lane >> 2) & 3, c4 = lane & 3;
       __syncthreads();
       const int have = min(KC, sets - first);
       constexpr int kS = (KC * QT + W - 1) / W, kL = KC * QT * 4 / W;
@@ -186,16 +216,30 @@ __global__ __launch_bounds__(W * 64, 2) void scores_kernel(ScoresArgs p) {
       __syncthreads();
     };
 
-    auto first_row = [&](long long tile) { return TAIL ? tile * ROWS : min(tile * ROWS, p.r.rows - ROWS); };
-    auto load = [&](RowSet<RB, RT>& a, long long tile, int set) {
-      const long long row0 = first_row(tile) + wave * (16 * RT);
+    // Where a lane's scale bytes of a set lie after its rows' first, and how far behind the address of a load of
+    // four that ends with the last row's last (at least four blocks lie in a tile).
+    auto scales_from = [&](int t, long long row0, int set, bool end) {
+      const unsigned at = (unsigned)(group * b4 + c4 + subtile(t)) * nb + set * 16 + (end ? end_steps : 4) * g;
+      const unsigned bytes = (unsigned)min((p.r.rows - row0) * nb, 0x7fffffffll), from = min(at, bytes - 4);
+      return make_uint2(from, at - from);
+    };
+    // Every p.turn tiles (a power of two) are passed over in an order of this query block's own.
+    const int n_tiles = (int)(t1 - t0), parts = n_tiles * PARTS, turn_of = (int)(q0 / (QT * 16)) & (p.turn - 1);
+    const int rest = n_tiles & (p.turn - 1), rest_of = rest ? turn_of % rest : 0;
+    auto first_row = [&](int part) {  // a wave's, of part `part` of the chunk's tiles
+      const int i = part / PARTS, from = i & -p.turn, many = from + rest == n_tiles && rest ? rest : p.turn;
+      int at = i - from + (many == p.turn ? turn_of : rest_of);
+      at = at >= many ? at - many : at;
+      const long long tile = t0 + from + at;
+      return (TAIL ? tile * ROWS : min(tile * ROWS, p.r.rows - ROWS)) + (wr * PARTS + part % PARTS) * (16 * RT);
+    };
+    auto load = [&](RowSet<RB, RT>& a, int part, int set) {
+      const long long row0 = first_row(part);
       const unsigned char* codes = p.r.codes + row0 * row_bytes + set * (64 * RB);
       const unsigned char* scales = p.r.scales + row0 * nb;
       const bool end = set == sets - 1;
       const int blk = end ? min(end_steps * g + min(c4, end_steps - 1), end_blocks - 1) : 4 * g + c4;
       const unsigned at = (unsigned)(group * b4) * row_bytes + (unsigned)blk * (4 * RB);
-      const unsigned from = (unsigned)(group * b4 + c4) * nb + set * 16 + (end ? end_steps : 4) * g;
-      const unsigned bytes = (unsigned)min((p.r.rows - row0) * nb, 0x7fffffffll);
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         if constexpr (TAIL) {
@@ -212,28 +256,33 @@ __global__ __launch_bounds__(W * 64, 2) void scores_kernel(ScoresArgs p) {
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i) load_block<RB>(a.w[t][i], codes + (at + (unsigned)(subtile(t) + i) * row_bytes));
-          a.s[t] = load_scales(scales, from + subtile(t) * nb, bytes);
+          __builtin_memcpy(&a.s[t], scales + scales_from(t, row0, set, end).x, 4);
         }
       }
     };
 
-    f32x4 acc[RT][QT];
-    auto product = [&](RowSet<RB, RT>& a, int set) {
+    f32x4 acc[RT][QW];
+    unsigned held[PAIR ? QW : 1][4];  // the first part of a tile, rounded
+    auto product = [&](RowSet<RB, RT>& a, int part, int set) {
       const int at = set % KC, steps = set == sets - 1 ? end_steps : 4;
       const int in = set == sets - 1 ? end_blocks - end_steps * g : 4;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         transpose4<RB>(a.w[t], c4 & 1, c4 & 2);
+        if constexpr (!TAIL) {
+          const long long row0 = first_row(part);
+          a.s[t] >>= 8 * min(scales_from(t, row0, set, set == sets - 1).y, 3u);
+        }
         a.s[t] = first_bytes(a.s[t], in);
       }
-      unsigned sb[QT];
+      unsigned sb[QW];
 #pragma unroll
-      for (int j = 0; j < QT; ++j) sb[j] = lds_s[(at * QT + j) * 64 + lane];
+      for (int j = 0; j < QW; ++j) sb[j] = lds_s[(at * QT + wq + j) * 64 + lane];
       auto one = [&](auto st) {
         constexpr int s = decltype(st)::value;
 #pragma unroll
-        for (int j = 0; j < QT; ++j) {
-          const int f = ((at * QT + j) * 16 + r16) * 16 + ((4 * g + s) ^ r16);
+        for (int j = 0; j < QW; ++j) {
+          const int f = ((at * QT + wq + j) * 16 + r16) * 16 + ((4 * g + s) ^ r16);
           unsigned b[QB];
           const uint4 lo = lds_lo[f];
           b[0] = lo.x, b[1] = lo.y, b[2] = lo.z, b[3] = lo.w;
@@ -250,14 +299,41 @@ __global__ __launch_bounds__(W * 64, 2) void scores_kernel(ScoresArgs p) {
       if (steps > 2) one(std::integral_constant<int, 2>{});
       if (steps > 3) one(std::integral_constant<int, 3>{});
     };
-    auto store = [&](long long tile) {
-      const long long row = first_row(tile) + wave * (16 * RT);
+    auto store = [&](int part) {
+      int lane = threadIdx.x & 63;
+      asm volatile("" : "+v"(lane));
+      const int r16 = lane & 15, g = lane >> 4;
+      const long long row = first_row(part);
+      if constexpr (PAIR) {
+        if (part % 2 == 0) {
 #pragma unroll
-      for (int j = 0; j < QT; ++j) {
-        const unsigned q = q0 + j * 16 + r16;
-        if (q > last_q) continue;
+          for (int j = 0; j < QW; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) held[j][i] = pack16(p.dtype, acc[i / 2][j][i % 2 * 2], acc[i / 2][j][i % 2 * 2 + 1]);
+          return;
+        }
+#pragma unroll
+        for (int j = 0; j < QW; ++j) {
+          unsigned lo[4], hi[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const unsigned v = pack16(p.dtype, acc[i / 2][j][i % 2 * 2], acc[i / 2][j][i % 2 * 2 + 1]);
+            lo[i] = swap_eight<0xc>(held[j][i], v);
+            hi[i] = swap_eight<0x3>(v, held[j][i]);
+          }
+          const unsigned ql = q0 + (wq + j) * 16 + (r16 & 7);
+          unsigned short* o = static_cast<unsigned short*>(p.out) + row - 32 + 4 * (r16 & 8) + 8 * g;
+          if (ql <= last_q) store_line(o + ql * p.ld, lo);
+          if (ql + 8 <= last_q) store_line(o + (ql + 8) * p.ld, hi);
+        }
+        return;
+      }
+#pragma unroll
+      for (int j = 0; j < QW; ++j) {
+        const unsigned q = q0 + (wq + j) * 16 + r16;
         const long long at = q * p.ld + row;
         if (p.dtype != kDtypeF32) {
+          if (q > last_q) continue;
           constexpr int N = RT > 1 ? 8 : 4;
 #pragma unroll
           for (int h = 0; h < 4 * RT / N; ++h) {
@@ -270,7 +346,25 @@ __global__ __launch_bounds__(W * 64, 2) void scores_kernel(ScoresArgs p) {
             else
               store_rows<TAIL>(static_cast<_Float16*>(p.out) + at + in, v, p.r.rows - row - in);
           }
-        } else {
+        } else if constexpr (RT % 2 == 0) {
+          // Whole cache lines: lanes of queries 0 .. 7 store both subtiles of these, the other eight lanes their second
+          // (taken from the lane eight below); then the same of queries 8 .. 15.
+#pragma unroll
+          for (int t = 0; t < RT; t += 2) {
+            float lo[4], hi[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const unsigned x = __float_as_uint(acc[t][j][i]), y = __float_as_uint(acc[t + 1][j][i]);
+              lo[i] = __uint_as_float(swap_eight<0xc>(x, y));
+              hi[i] = __uint_as_float(swap_eight<0x3>(y, x));
+            }
+            const unsigned ql = q0 + (wq + j) * 16 + (r16 & 7);
+            const long long in = row + 16 * t + 2 * (r16 & 8) + 4 * g;
+            float* o = static_cast<float*>(p.out) + in;
+            if (ql <= last_q) store_rows<TAIL>(o + ql * p.ld, lo, p.r.rows - in);
+            if (ql + 8 <= last_q) store_rows<TAIL>(o + (ql + 8) * p.ld, hi, p.r.rows - in);
+          }
+        } else if (q <= last_q) {
 #pragma unroll
           for (int t = 0; t < RT; ++t) {
             const float v[4] = {acc[t][j][0], acc[t][j][1], acc[t][j][2], acc[t][j][3]};
@@ -281,7 +375,7 @@ __global__ __launch_bounds__(W * 64, 2) void scores_kernel(ScoresArgs p) {
     };
 
     // Sets of all tiles one after the other, each loaded while the one before it is multiplied.
-    long long tile = t0, next_tile = t0;
+    int part = 0, next_part = 0;
     int set = 0, next_set = 0;
     RowSet<RB, RT> x, y;
     auto turn = [&](RowSet<RB, RT>& cur, RowSet<RB, RT>& next) {
@@ -289,43 +383,52 @@ __global__ __launch_bounds__(W * 64, 2) void scores_kernel(ScoresArgs p) {
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
-          for (int j = 0; j < QT; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int j = 0; j < QW; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
       if (!RES && set % KC == 0) stage(set);
-      if (++next_set == sets) next_set = 0, next_tile = min(next_tile + 1, t1 - 1);  // past the end: loaded, not used
-      load(next, next_tile, next_set);
+      if (++next_set == sets) next_set = 0, next_part = min(next_part + 1, parts - 1);  // past the end: loaded, not used
+      load(next, next_part, next_set);
       __builtin_amdgcn_sched_barrier(0);
-      product(cur, set);
+      product(cur, part, set);
       if (++set == sets) {
-        store(tile);
+        store(part);
         set = 0;
-        ++tile;
+        ++part;
       }
     };
-    load(x, tile, 0);
+    load(x, 0, 0);
     if constexpr (RES) stage(0);
-    for (;;) {
+    // (No way out of the middle of the loop: the waits of a turn would have to hold for it too.)
+    const long long turns = (long long)parts * sets;
+    for (long long i = turns / 2; i > 0; --i) {
       turn(x, y);
-      if (tile >= t1) break;
       turn(y, x);
-      if (tile >= t1) break;
     }
+    if (turns & 1) turn(x, y);
   }
 }
 
-template <int QB, int RB, int W, int RT, int QT, bool RES, bool TAIL = false>
+template <int QB, int RB, int W, int WQ, int RT, int QT, bool RES, bool PAIR = false, bool TAIL = false>
 hipError_t launch(ScoresArgs p, hipStream_t s) {
   p.n_qblocks = (int)((p.q.rows + 16 * QT - 1) / (16 * QT));
-  const int tiles = (int)((p.r.rows + W * RT * 16 - 1) / (W * RT * 16));
+  constexpr int kRows = W / WQ * (PAIR ? 2 : 1) * RT * 16;
+  if (!TAIL && p.r.rows < kRows) return hipErrorInvalidValue;
+  const int tiles = (int)((p.r.rows + kRows - 1) / kRows);
   // Eight waves per CU.
   const int most = 2048 / W;
   p.n_chunks = std::max(1, std::min(tiles, most / std::min(p.n_qblocks, most)));
   p.least = tiles / p.n_chunks;
   p.spare = tiles % p.n_chunks;
   const long long items = (long long)p.n_qblocks * p.n_chunks;
+  // All query blocks of a chunk that wait for the same tile wait for memory every time; in turned orders each tile is
+  // in their L2 after the first one's wait.  As long as that holds them all: 3.5 of its 4 MB, the chunks of 32 CUs.
+  // (1,024 x 262,144 x 768, 6 and 4 bits to bf16: in one order 342 us, of 2 tiles 330, of 4 325, of 8 288, of 16 326.)
+  const long long bytes = (long long)kRows * p.r.nb * (4 * RB + 1) * std::max(1, 32 / p.n_qblocks);
+  p.turn = 1;
+  while (p.turn < 8 && 2 * p.turn <= p.n_qblocks && 2 * p.turn * bytes <= 7 << 19) p.turn *= 2;
   const int kc = std::min(lds_sets<QT>(), (p.r.nb + 15) / 16);
   const unsigned lds = (unsigned)(kc * QT * (256 * 4 * QB + 64 * 4));
-  scores_kernel<QB, RB, W, RT, QT, RES, TAIL><<<(unsigned)std::min<long long>(items, 1 << 20), W * 64, lds, s>>>(p);
+  scores_kernel<QB, RB, W, WQ, RT, QT, RES, PAIR, TAIL><<<(unsigned)std::min<long long>(items, 1 << 20), W * 64, lds, s>>>(p);
   return hipGetLastError();
 }
 
@@ -341,12 +444,23 @@ hipError_t launch_mx_scores(const MxRows& q, const MxRows& rows, void* out, int 
   const int sets = (q.nb + 15) / 16;
   return with_bits(q.bits, [&](auto qb) {
     return with_bits(rows.bits, [&](auto rb) {
-      constexpr int RT = rb() == 4 ? 2 : 1;  // (6 bits: a set of two subtiles takes too many registers)
-      if (rows.rows < 128) return launch<qb(), rb(), 8, 1, 4, false, true>(p, s);
-      if (q.rows <= 16 && sets <= lds_sets<1>()) return launch<qb(), rb(), 4, 1, 1, true>(p, s);
-      if (q.rows > 64 && sets <= lds_sets<8>() && rows.rows >= 128 * RT) return launch<qb(), rb(), 8, RT, 8, true>(p, s);
-      if (sets <= lds_sets<4>()) return launch<qb(), rb(), 8, 1, 4, true>(p, s);
-      return launch<qb(), rb(), 8, 1, 4, false>(p, s);
+      constexpr int WQ = rb() == 4 ? 1 : 2, kLarge = 8 / WQ * 2 * 16;  // (6-bit rows: registers)
+      const bool pairs = dtype != kDtypeF32;
+      // Whether tiles of so many queries and rows give every CU one.  Where they do not, smaller ones are faster: 77 x
+      // 10,007 x 384 to bf16 in parts 15.1 us, not 10.5, 64 x 10,007 x 768 by two subtiles 16.7, not 9.0; where they
+      // do, larger ones: 64 x 10^6 x 768 228 us and 114, 1,024 x 262,144 (6 bits both) 384 us and 328.
+      auto fill = [&](int tile_q, int tile_r) { return (q.rows + tile_q - 1) / tile_q * (rows.rows / tile_r) >= 256; };
+      if (rows.rows < 128) return launch<qb(), rb(), 8, 1, 1, 4, false, false, true>(p, s);
+      if (q.rows <= 16 && sets <= lds_sets<1>()) return launch<qb(), rb(), 4, 1, 1, 1, true>(p, s);
+      if (q.rows > 64 && sets <= lds_sets<8>() && rows.rows >= kLarge) {
+        if (pairs && fill(128, 2 * kLarge)) return launch<qb(), rb(), 8, WQ, 2, 8, true, true>(p, s);
+        return launch<qb(), rb(), 8, WQ, 2, 8, true>(p, s);
+      }
+      if (sets <= lds_sets<4>()) {
+        if (!fill(64, 512)) return launch<qb(), rb(), 8, 1, 1, 4, true>(p, s);
+        return pairs ? launch<qb(), rb(), 8, 1, 2, 4, true, true>(p, s) : launch<qb(), rb(), 8, 1, 2, 4, true>(p, s);
+      }
+      return launch<qb(), rb(), 8, 1, 1, 4, false>(p, s);
     });
   });
 }
