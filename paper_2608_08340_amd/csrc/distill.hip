@@ -318,6 +318,7 @@ __global__ __launch_bounds__(T + 64, V == 64 ? 5 : 4) void row_kernel(Args p) {
     Entries e;
     if (GRAD) clear(set);
     e.begin<DT>(a, q, 0, a.n, w);
+    if (GRAD && a.grad == a.logits) drain();  // the entries' logits, before the others store over them
     lds_barrier();
     e.finish(a, 0, set);
     lds_barrier();
@@ -482,7 +483,7 @@ __global__ __launch_bounds__(kPieceThreads + 64) void grad_kernel(Args p) {
     Entries e;
     clear(rows);
     e.begin<DT>(a, q, i0, i1, w);
-    if (LSE && a.grad == a.logits) drain();  // the entries' logits, before the others store over them
+    if (a.grad == a.logits) drain();  // the entries' logits, before the others store over them
     lds_barrier();
     e.finish(a, i0, rows);
     if constexpr (LSE) {

@@ -44,6 +44,7 @@ struct GradArgs {
   float* part;       // [splits][m][pitch], or null
   long long pitch;
   int m_tiles, d_tiles, splits;
+  int first_tile;    // the launch's first tile of m
   int per;           // stages of a split
 };
 
@@ -97,7 +98,8 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs p) {
   const int wm = wave / WD, wd = wave % WD;
 
   const unsigned L = (unsigned)logical_block();
-  const int di0 = (int)(L % p.d_tiles), mi0 = (int)(L / p.d_tiles % p.m_tiles), split = (int)(L / p.d_tiles / p.m_tiles);
+  const int di0 = (int)(L % p.d_tiles), mi0 = p.first_tile + (int)(L / p.d_tiles % p.m_tiles);
+  const int split = (int)(L / p.d_tiles / p.m_tiles);
   // The last tile of a transposed G ends with its last column, and makes some rows of out that the tile before it has
   // too, to the same bits.
   const long long m0 = TRANS && !EDGE ? min((long long)mi0 * BM, p.m - BM) : (long long)mi0 * BM;
@@ -473,13 +475,18 @@ GradPlan plan_grad(long long m, const MxRows& x) {
 }
 long long part_pitch(const MxRows& x) { return (x.dim + 3) & ~3; }
 
+// (A launch holds fewer than 2^32 threads: 2^22 workgroups each, which only an unsplit k can pass.)
 template <int DT, int BITS, bool TRANS, int BM, bool EDGE>
-hipError_t launch_tiles(const GradArgs& a, hipStream_t s) {
+hipError_t launch_tiles(GradArgs a, hipStream_t s) {
   constexpr unsigned lds = 2 * (kXBytes + planes<DT>() * BM * kBK * 2);
   static_assert(lds <= 163840, "LDS");
-  const long long grid = (long long)a.m_tiles * a.d_tiles * a.splits;
-  grad_kernel<DT, BITS, TRANS, BM, EDGE><<<(unsigned)grid, kThreads, lds, s>>>(a);
-  return hipGetLastError();
+  const int all = a.m_tiles, most = (1 << 22) / (a.d_tiles * a.splits);
+  for (a.first_tile = 0; a.first_tile < all; a.first_tile += most) {
+    a.m_tiles = std::min(most, all - a.first_tile);
+    grad_kernel<DT, BITS, TRANS, BM, EDGE><<<(unsigned)(a.m_tiles * a.d_tiles * a.splits), kThreads, lds, s>>>(a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

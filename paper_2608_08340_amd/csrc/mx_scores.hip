@@ -68,7 +68,9 @@ __device__ __forceinline__ void load_block(unsigned (&w)[BITS], const unsigned c
   }
 }
 
-// The n bytes (1 to 4) from p on, by the aligned words that hold the first and the last of them.
+// The n bytes (1 to 4) from p on, by the aligned words that hold the first and the last of them.  (A word may pass the
+// array's end by up to three bytes, which are not used; it lies within 16 bytes of the array's alignment, so no page
+// is read that the array does not have.)
 __device__ __forceinline__ unsigned load_bytes(const unsigned char* p, int n) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p);
   const unsigned lo = *reinterpret_cast<const unsigned*>(a & ~uintptr_t(3));
