@@ -359,14 +359,18 @@ def time_next_dense_kernel(start: torch.cuda.Event | None, stop: torch.cuda.Even
 
 
 # ---------------------------------------------------------------------- rows in few bits
+# Small calls take as long as the host does to make them: one query of 1,024 elements quantised in 11.8 us with a
+# stream object, ctypes pointers and every check made again of what the call itself has allocated, in 8.4 without.
 def _run(device: torch.device, name: str, *args) -> None:
     """Calls the library on `device`'s current stream (the last argument of every such call)."""
-    fn = getattr(library(), name)
+    fn = getattr(_lib or library(), name)
     if torch.cuda.current_device() == device.index:
-        _check(fn(*args, _stream(device)))
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, _stream(device)))
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if status != 0:
+        _check(status)
 
 
 def _on_gpu(device: torch.device) -> torch.device:
@@ -377,15 +381,17 @@ def _on_gpu(device: torch.device) -> torch.device:
 
 def _matrix(t: torch.Tensor, device, shape, name: str, dtype=None) -> int:
     """The row stride of a row-major matrix, checked."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.device != device:
+    if not isinstance(t, torch.Tensor) or len(t.shape) != 2 or t.device != device:
         raise OpragError(-1, f"{name} must be a matrix on {device}")
     if t.dtype not in _DTYPE or (dtype is not None and t.dtype != dtype):
         raise OpragError(-1, f"unsupported {name} dtype {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise OpragError(-1, f"{name} must be {list(shape)}, not {list(t.shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    n, d = shape
+    row, col = t.stride()
+    if d > 1 and col != 1:
         raise OpragError(-1, f"{name} must have contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(1, t.shape[1])
+    return row if n > 1 else max(1, d)
 
 
 class MxRows:
@@ -397,44 +403,46 @@ class MxRows:
     of some of the rows, to append to or to score a shard of.
     """
 
-    __slots__ = ("codes", "scales", "dim", "bits", "first", "n")
+    __slots__ = ("codes", "scales", "dim", "bits", "first", "n", "device")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, dim: int, first: int = 0, n: int | None = None):
         dim = int(dim)
         nb = (dim + 31) // 32
-        if codes.dim() != 3 or codes.shape[2] not in (16, 24) or codes.shape[1] != nb:
-            raise OpragError(-1, f"codes must be [n, {nb}, 16 or 24] for dim {dim}, not {list(codes.shape)}")
-        if tuple(scales.shape) != tuple(codes.shape[:2]):
-            raise OpragError(-1, f"scales must be {list(codes.shape[:2])}, not {list(scales.shape)}")
-        _dev_tensor(codes, torch.uint8, codes.device, "codes")
-        _dev_tensor(scales, torch.uint8, codes.device, "scales")
-        n = codes.shape[0] - first if n is None else n
-        if first < 0 or n < 0 or first + n > codes.shape[0]:
-            raise OpragError(-1, f"rows [{first}, {first + n}) outside [0, {codes.shape[0]})")
-        self.codes, self.scales, self.dim, self.bits = codes, scales, dim, codes.shape[2] // 4
-        self.first, self.n = first, n
+        shape, device = codes.shape, codes.device
+        if len(shape) != 3 or shape[2] not in (16, 24) or shape[1] != nb:
+            raise OpragError(-1, f"codes must be [n, {nb}, 16 or 24] for dim {dim}, not {list(shape)}")
+        if scales.shape != shape[:2]:
+            raise OpragError(-1, f"scales must be {list(shape[:2])}, not {list(scales.shape)}")
+        _dev_tensor(codes, torch.uint8, device, "codes")
+        _dev_tensor(scales, torch.uint8, device, "scales")
+        n = shape[0] - first if n is None else n
+        if first < 0 or n < 0 or first + n > shape[0]:
+            raise OpragError(-1, f"rows [{first}, {first + n}) outside [0, {shape[0]})")
+        self._set(codes, scales, dim, shape[2] // 4, first, n, device)
+
+    def _set(self, codes, scales, dim, bits, first, n, device):
+        self.codes, self.scales, self.dim, self.bits = codes, scales, dim, bits
+        self.first, self.n, self.device = first, n, device
+        return self
 
     @classmethod
     def empty(cls, n: int, dim: int, bits: int = 4, device: int | torch.device = 0) -> "MxRows":
         if bits not in (4, 6):
             raise OpragError(-1, f"bits = {bits} is not 4 or 6")
         dev = torch.device("cuda", device) if isinstance(device, int) else device
-        nb = (int(dim) + 31) // 32
-        return cls(torch.empty((n, nb, 4 * bits), dtype=torch.uint8, device=dev),
-                   torch.empty((n, nb), dtype=torch.uint8, device=dev), dim)
+        dim = int(dim)
+        nb = (dim + 31) // 32
+        codes = torch.empty((n, nb, 4 * bits), dtype=torch.uint8, device=dev)
+        return cls.__new__(cls)._set(codes, codes.new_empty((n, nb)), dim, bits, 0, n, codes.device)
 
     def part(self, first: int, n: int) -> "MxRows":
         """Rows [first, first + n), sharing this object's memory."""
         if first < 0 or n < 0 or first + n > self.n:
             raise OpragError(-1, f"rows [{first}, {first + n}) outside [0, {self.n})")
-        return MxRows(self.codes, self.scales, self.dim, self.first + first, n)
+        return MxRows.__new__(MxRows)._set(self.codes, self.scales, self.dim, self.bits, self.first + first, n, self.device)
 
     def __len__(self) -> int:
         return self.n
-
-    @property
-    def device(self) -> torch.device:
-        return self.codes.device
 
     def _desc(self) -> _MxDesc:
         return _MxDesc(self.codes.data_ptr(), self.scales.data_ptr(), self.first, self.n, self.dim, self.bits)
@@ -446,27 +454,39 @@ def _mx(rows, device, name: str) -> MxRows:
     return rows
 
 
+def _output(out, dev, shape, dtype):
+    """`out`, checked, or a new matrix, and its row stride."""
+    if out is not None:
+        return out, _matrix(out, dev, shape, "out", dtype)
+    if dtype not in _DTYPE:
+        raise OpragError(-1, f"unsupported out dtype {dtype}")
+    return torch.empty(shape, dtype=dtype, device=dev), max(1, shape[1])
+
+
+def _workspace(dev, need: ctypes.c_size_t):
+    size = need.value
+    return (torch.empty(size, dtype=torch.uint8, device=dev) if size else None), size
+
+
 def mx_quantize(x: torch.Tensor, bits: int = 4, out: MxRows | None = None) -> MxRows:
     """Quantises rows [n x dim] (fp32, bf16 or fp16; rows may be strided), into `out` if given."""
-    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+    if not isinstance(x, torch.Tensor) or len(x.shape) != 2:
         raise OpragError(-1, "x must be a matrix")
-    _on_gpu(x.device)
-    ld = _matrix(x, x.device, x.shape, "x")
+    dev = _on_gpu(x.device)
+    ld = _matrix(x, dev, x.shape, "x")
     if out is None:
-        out = MxRows.empty(x.shape[0], x.shape[1], bits, x.device)
-    elif len(_mx(out, x.device, "out")) != x.shape[0] or out.dim != x.shape[1] or out.bits != bits:
+        out = MxRows.empty(x.shape[0], x.shape[1], bits, dev)
+    elif len(_mx(out, dev, "out")) != x.shape[0] or out.dim != x.shape[1] or out.bits != bits:
         raise OpragError(-1, f"out must hold {x.shape[0]} rows of {x.shape[1]} elements in {bits} bits")
-    _run(x.device, "oprag_mx_quantize", _ptr(x), _DTYPE[x.dtype], ld, out._desc())
+    _run(dev, "oprag_mx_quantize", x.data_ptr(), _DTYPE[x.dtype], ld, out._desc())
     return out
 
 
 def mx_values(rows: MxRows, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values that quantised rows stand for, [n x dim]."""
     dev = _on_gpu(_mx(rows, getattr(rows, "device", None), "rows").device)
-    if out is None:
-        out = torch.empty((len(rows), rows.dim), dtype=dtype, device=dev)
-    ld = _matrix(out, dev, (len(rows), rows.dim), "out", dtype)
-    _run(dev, "oprag_mx_values", rows._desc(), _ptr(out), _DTYPE[dtype], ld)
+    out, ld = _output(out, dev, (rows.n, rows.dim), dtype)
+    _run(dev, "oprag_mx_values", rows._desc(), out.data_ptr(), _DTYPE[dtype], ld)
     return out
 
 
@@ -475,10 +495,8 @@ def mx_scores(q: MxRows, rows: MxRows, dtype: torch.dtype = torch.float32,
     """Inner products [len(q) x len(rows)], summed in fp32, in `dtype`."""
     dev = _on_gpu(_mx(q, getattr(q, "device", None), "q").device)
     _mx(rows, dev, "rows")
-    if out is None:
-        out = torch.empty((len(q), len(rows)), dtype=dtype, device=dev)
-    ld = _matrix(out, dev, (len(q), len(rows)), "out", dtype)
-    _run(dev, "oprag_mx_scores", q._desc(), rows._desc(), _ptr(out), _DTYPE[dtype], ld)
+    out, ld = _output(out, dev, (q.n, rows.n), dtype)
+    _run(dev, "oprag_mx_scores", q._desc(), rows._desc(), out.data_ptr(), _DTYPE[dtype], ld)
     return out
 
 
@@ -487,40 +505,40 @@ def mx_scores_grad(grad: torch.Tensor, x: MxRows, transposed: bool = False,
     """The gradient of ``mx_scores``, straight through the quantisation, fp32: to the queries grad @
     values(x) with x the rows, or, transposed, to the rows grad.T @ values(x) with x the queries."""
     dev = _on_gpu(_mx(x, getattr(x, "device", None), "x").device)
-    if not isinstance(grad, torch.Tensor) or grad.dim() != 2:
+    if not isinstance(grad, torch.Tensor) or len(grad.shape) != 2:
         raise OpragError(-1, "grad must be a matrix")
     m = grad.shape[1] if transposed else grad.shape[0]
-    ld = _matrix(grad, dev, (len(x), m) if transposed else (m, len(x)), "grad")
-    if out is None:
-        out = torch.empty((m, x.dim), dtype=torch.float32, device=dev)
-    out_ld = _matrix(out, dev, (m, x.dim), "out", torch.float32)
+    ld = _matrix(grad, dev, (x.n, m) if transposed else (m, x.n), "grad")
+    out, out_ld = _output(out, dev, (m, x.dim), torch.float32)
     desc, need = x._desc(), ctypes.c_size_t()
-    _check(library().oprag_mx_scores_grad_bytes(m, desc, ctypes.byref(need)))
-    ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
-    _run(dev, "oprag_mx_scores_grad", _ptr(grad), _DTYPE[grad.dtype], ld, int(transposed), m, desc, _ptr(out), out_ld,
-                                          _ptr(ws), need.value)
+    _check(library().oprag_mx_scores_grad_bytes(m, desc, need))
+    ws, size = _workspace(dev, need)
+    _run(dev, "oprag_mx_scores_grad", grad.data_ptr(), _DTYPE[grad.dtype], ld, int(transposed), m, desc, out.data_ptr(),
+         out_ld, None if ws is None else ws.data_ptr(), size)
     return out
 
 
 # ---------------------------------------------------------------------- distillation
 def _distill_args(logits, teacher_ids, teacher_scores, temperature, teacher_temperature):
-    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+    if not isinstance(logits, torch.Tensor) or len(logits.shape) != 2:
         raise OpragError(-1, "logits must be a matrix")
     dev = _on_gpu(logits.device)
     ld = _matrix(logits, dev, logits.shape, "logits")
     _dev_tensor(teacher_ids, torch.int64, dev, "teacher_ids")
     _dev_tensor(teacher_scores, torch.float32, dev, "teacher_scores")
     nq, n = logits.shape
-    if teacher_ids.dim() != 2 or teacher_ids.shape[0] != nq or teacher_scores.shape != teacher_ids.shape:
+    shape = teacher_ids.shape
+    if len(shape) != 2 or shape[0] != nq or teacher_scores.shape != shape:
         raise OpragError(-1, f"teacher_ids and teacher_scores must both be [{nq} x k]")
-    return dev, (_ptr(logits), _DTYPE[logits.dtype], ld, nq, n, _ptr(teacher_ids), _ptr(teacher_scores),
-                 teacher_ids.shape[1], temperature, teacher_temperature)
+    return dev, (logits.data_ptr(), _DTYPE[logits.dtype], ld, nq, n, teacher_ids.data_ptr(), teacher_scores.data_ptr(),
+                 shape[1], temperature, teacher_temperature)
 
 
 def _distill_ws(dev, nq: int, n: int):
     need = ctypes.c_size_t()
-    _check(library().oprag_distill_bytes(nq, n, ctypes.byref(need)))
-    return (torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None), need.value
+    _check(library().oprag_distill_bytes(nq, n, need))
+    ws, size = _workspace(dev, need)
+    return ws, (None if ws is None else ws.data_ptr()), size
 
 
 def _vector(t, n: int, dev, name: str) -> torch.Tensor:
@@ -537,9 +555,9 @@ def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_scores
     dev, a = _distill_args(logits, teacher_ids, teacher_scores, temperature, teacher_temperature)
     nq, n = logits.shape
     loss = torch.empty(nq, dtype=torch.float32, device=dev)
-    lse = torch.empty(nq, dtype=torch.float32, device=dev)
-    ws, size = _distill_ws(dev, nq, n)
-    _run(dev, "oprag_distill_loss", *a, _ptr(loss), _ptr(lse), _ptr(ws), size)
+    lse = torch.empty_like(loss)
+    ws, at, size = _distill_ws(dev, nq, n)
+    _run(dev, "oprag_distill_loss", *a, loss.data_ptr(), lse.data_ptr(), at, size)
     return loss, lse
 
 
@@ -551,9 +569,8 @@ def distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_scores
     nq, n = logits.shape
     _vector(lse, nq, dev, "lse")
     _vector(weight, nq, dev, "weight")
-    out = torch.empty((nq, n), dtype=logits.dtype, device=dev) if out is None else out
-    out_ld = _matrix(out, dev, (nq, n), "out", logits.dtype)
-    _run(dev, "oprag_distill_grad", *a, _ptr(lse), _ptr(weight), _ptr(out), out_ld)
+    out, out_ld = _output(out, dev, (nq, n), logits.dtype)
+    _run(dev, "oprag_distill_grad", *a, lse.data_ptr(), weight.data_ptr(), out.data_ptr(), out_ld)
     return out
 
 
@@ -564,8 +581,7 @@ def distill_step(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_scores
     nq, n = logits.shape
     _vector(weight, nq, dev, "weight")
     loss = torch.empty(nq, dtype=torch.float32, device=dev)
-    out = torch.empty((nq, n), dtype=logits.dtype, device=dev) if out is None else out
-    out_ld = _matrix(out, dev, (nq, n), "out", logits.dtype)
-    ws, size = _distill_ws(dev, nq, n)
-    _run(dev, "oprag_distill_step", *a, _ptr(weight), _ptr(loss), _ptr(out), out_ld, _ptr(ws), size)
+    out, out_ld = _output(out, dev, (nq, n), logits.dtype)
+    ws, at, size = _distill_ws(dev, nq, n)
+    _run(dev, "oprag_distill_step", *a, weight.data_ptr(), loss.data_ptr(), out.data_ptr(), out_ld, at, size)
     return loss, out
