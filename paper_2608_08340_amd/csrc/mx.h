@@ -49,6 +49,12 @@ __device__ __forceinline__ void store_from_f32(void* p, long long i, float v) {
   }
 }
 
+// `keep`, and in the lanes whose group of four within sixteen MASK names `take` of the lane eight away.
+template <int MASK>
+__device__ __forceinline__ unsigned swap_eight(unsigned keep, unsigned take) {
+  return (unsigned)__builtin_amdgcn_update_dpp((int)keep, (int)take, 0x128, 0xf, MASK, false);
+}
+
 }  // namespace dev
 
 // Calls f(std::integral_constant<int, dtype>) for a run-time dtype.

@@ -107,12 +107,6 @@ __device__ __forceinline__ void transpose4(unsigned (&w)[4][RB], bool odd, bool 
   }
 }
 
-// `keep`, and in the lanes whose group of four within sixteen MASK names `take` of the lane eight away.
-template <int MASK>
-__device__ __forceinline__ unsigned swap_eight(unsigned keep, unsigned take) {
-  return (unsigned)__builtin_amdgcn_update_dpp((int)keep, (int)take, 0x128, 0xf, MASK, false);
-}
-
 // Two sums in a 16-bit type.
 __device__ __forceinline__ unsigned pack16(int dtype, float a, float b) {
   typedef __bf16 B2 __attribute__((ext_vector_type(2)));
