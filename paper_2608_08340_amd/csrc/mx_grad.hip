@@ -19,7 +19,7 @@
 //
 // Measured (4 bits, to the queries unless said): of an fp32 G, 1,024 x 32,768 x 1,024 171 us, the three planes' products
 // at 1.2 PFLOP/s, 89 % of what a large library product in bf16 reaches; of bf16 81 us, of 16 rows (fp32) 15.5; the
-// rows' gradient of bf16, 1,000 x 20,011 x 768 (6 bits) 46 us, the products at 0.66 PFLOP/s: one round of tiles, whose
+// rows' gradient of bf16, 1,000 x 20,011 x 768 (6 bits) 43 us, the products at 0.71 PFLOP/s: one round of tiles, whose
 // first loads and last stores nothing hides.  One row over 100,003 x 384 (fp16) 7.4 us and 3.6 for the join.  Bound by the
 // matrix instructions and, for 16-bit G, by the stages' own steps (decode, LDS).  (Half of the waves multiplying first and
 // then writing, against the other half: 171 -> 185 us, 46 -> 74.)
@@ -137,18 +137,21 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs p) {
   };
   // Piece i of G: its row and column in the stage.  Rows past m are read from the last one and not stored.
   auto piece = [&](int i) { return min(tid + i * kThreads, kChunks - 1); };
-  const T* g_at[kG];
+  // (Of a transposed G they lie a number of its rows apart: one address serves.)
+  constexpr int kAddresses = TRANS && kThreads % kRow == 0 && kChunks % kThreads == 0 ? 1 : kG;
+  const T* g_first[kAddresses];
 #pragma unroll
-  for (int i = 0; i < kG; ++i) {
+  for (int i = 0; i < kAddresses; ++i) {
     const int row = piece(i) / kRow, col = piece(i) % kRow * EV;
-    g_at[i] = static_cast<const T*>(p.g) +
+    g_first[i] = static_cast<const T*>(p.g) +
               (TRANS ? (k_first + row) * p.ld + m0 + col : min(m0 + row, p.m - 1) * p.ld + k_first + col);
   }
+  auto g_at = [&](int i) { return kAddresses == kG ? g_first[min(i, kAddresses - 1)] : g_first[0] + i * (kThreads / kRow) * p.ld; };
   const long long g_step = TRANS ? kBK * p.ld : kBK;
   auto load_whole = [&](Share& a, int stage) {  // a stage with all its k
     load_codes(a, x_at + (long long)stage * kBK * p.x.nb);
 #pragma unroll
-    for (int i = 0; i < kG; ++i) a.g[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const V*>(g_at[i] + stage * g_step));
+    for (int i = 0; i < kG; ++i) a.g[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const V*>(g_at(i) + stage * g_step));
     __builtin_amdgcn_sched_barrier(0);  // loads stay in their order: the wait for one leaves those after it in flight
   };
   auto load_some = [&](Share& a, int stage) {
@@ -163,10 +166,10 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs p) {
       const long long in = TRANS ? (k0 + row < K ? p.m - m0 - col : 0) : K - k0 - col;
       V v;
       if (in >= EV) {
-        v = *reinterpret_cast<const V*>(g_at[i] + stage * g_step);
+        v = *reinterpret_cast<const V*>(g_at(i) + stage * g_step);
       } else {
 #pragma unroll
-        for (int e = 0; e < EV; ++e) v[e] = e < in ? g_at[i][stage * g_step + e] : (T)0;
+        for (int e = 0; e < EV; ++e) v[e] = e < in ? g_at(i)[stage * g_step + e] : (T)0;
       }
       a.g[i] = __builtin_bit_cast(u32x4, v);
     }
@@ -243,30 +246,46 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs p) {
   auto product = [&](const unsigned char* buf) {
 #pragma unroll
     for (int ks = 0; ks < kBK / 32; ++ks) {
-      bf16x8 xf[DI];
-#pragma unroll
-      for (int i = 0; i < DI; ++i) {
+      auto x_piece = [&](int i) {
         const unsigned char* at = buf + (ks * 32 + tr_row) * (kBD * 2) + ((wd * DI + i) ^ tr_mix ^ ((wd * DI + i) >> 3)) * 32 + tr_col;
         const bf16x4 a = tr_read(at), b = tr_read(at + 4 * (kBD * 2));
-        xf[i] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-#pragma unroll
-      for (int pl = 0; pl < P; ++pl) {
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      auto g_piece = [&](int pl, int j) {
         const unsigned char* gb = buf + kXBytes + pl * kGBytes;
+        if constexpr (TRANS) {
+          const unsigned char* at =
+              gb + (ks * 32 + tr_row) * (BM * 2) + ((wm * MI + j) ^ (tr_mix & kMix)) * 32 + tr_col;
+          const bf16x4 a = tr_read(at), b = tr_read(at + 4 * (BM * 2));
+          return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+          const int m = (wm * MI + j) * 16 + r16;
+          return *reinterpret_cast<const bf16x8*>(gb + m * (kBK * 2) + ((ks * 4 + g4) ^ ((m >> 1) & 7)) * 16);
+        }
+      };
+      // The shorter side stays in registers, but for G's planes.
+      if constexpr (P == 1 && DI > MI) {
+        bf16x8 gf[MI];
 #pragma unroll
-        for (int j = 0; j < MI; ++j) {
-          bf16x8 gf;
-          if constexpr (TRANS) {
-            const unsigned char* at =
-                gb + (ks * 32 + tr_row) * (BM * 2) + ((wm * MI + j) ^ (tr_mix & kMix)) * 32 + tr_col;
-            const bf16x4 a = tr_read(at), b = tr_read(at + 4 * (BM * 2));
-            gf = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-          } else {
-            const int m = (wm * MI + j) * 16 + r16;
-            gf = *reinterpret_cast<const bf16x8*>(gb + m * (kBK * 2) + ((ks * 4 + g4) ^ ((m >> 1) & 7)) * 16);
+        for (int j = 0; j < MI; ++j) gf[j] = g_piece(0, j);
+#pragma unroll
+        for (int i = 0; i < DI; ++i) {
+          const bf16x8 xf = x_piece(i);
+#pragma unroll
+          for (int j = 0; j < MI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, gf[j], acc[i][j], 0, 0, 0);
+        }
+      } else {
+        bf16x8 xf[DI];
+#pragma unroll
+        for (int i = 0; i < DI; ++i) xf[i] = x_piece(i);
+#pragma unroll
+        for (int pl = 0; pl < P; ++pl) {
+#pragma unroll
+          for (int j = 0; j < MI; ++j) {
+            const bf16x8 gf = g_piece(pl, j);
+#pragma unroll
+            for (int i = 0; i < DI; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[i], gf, acc[i][j], 0, 0, 0);
           }
-#pragma unroll
-          for (int i = 0; i < DI; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[i], gf, acc[i][j], 0, 0, 0);
         }
       }
     }
