@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("n", [4095, 4096, 4097, 8193, 16383, 16384, 16385, 32767, 32768, 32769, 40961])
+@pytest.mark.parametrize("n", [4095, 4096, 4097, 8191, 8192, 8193, 24575, 24576, 24577, 16383, 16384, 16385, 32767, 32768, 32769, 40961])
 def test_distill_at_the_ends_of_a_row_or_piece(dtype, n):
     log("distill", dtype, n)
     run_all(*draw(n, 3, n, 20, dtype), 0.05, 0.5, dtype, (dtype, n))
