@@ -17,6 +17,10 @@
 // Every workgroup has one wave more than its elements need: it makes the teacher (dependent loads and fp64
 // logarithms, about as long as the others take to load and reduce) and the loss, and stores the
 // entries.  (By a wave with elements of its own, before or after them: 1,024 x 32,768 fp32 89 us.)
+//
+// Measured, the step (bytes read and written once): 1,024 x 32,768 of fp32 55 us, 4.8 TB/s (a large copy: 4.76), of bf16 36 us,
+// 3.7 TB/s (two rounds of workgroups, whose conversions and exponentials memory waits for); 1,024 x 20,000 of fp32 33 us;
+// 32 x 1,000,000 of fp32 61 us, 4.2 TB/s over two reads.  The loss alone of 1,024 x 32,768 31 and 22 us.
 #include <algorithm>
 #include <cmath>
 

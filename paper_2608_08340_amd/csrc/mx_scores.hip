@@ -19,11 +19,12 @@
 // parts of a tile (PAIR; the first waits in registers): stores of half lines alone take 185 us for 537 MB,
 // of whole ones 119.
 //
-// Measured, rows and sums read and written once: 1,024 x 262,144 x 768 (6 and 4 bits) to bf16 256 us, 2.5 TB/s, 1.6
-// PFLOP/s; to fp32 287 us, 4.1 TB/s; 128 x 2,000,000 x 768 to bf16 286 us, 4.6 TB/s; 256 x 32,768 x 1,024 to
-// fp32 17 us, 3.0 TB/s; 1,024 x 32,768 x 4,096 (queries do not fit LDS) to bf16 214 us, 1.3 PFLOP/s.
-// Without its stores the first takes 187 us, without its loads 228: bound by the memory's latency under stores, of
-// which two sets in flight hide a part, and by LDS, from which every product reads its queries.  Three or
+// Measured, three sets of rows and sums in turn: 1,024 x 262,144 x 768 (queries 6, rows 4 bits) to bf16 215 to 226 us, 2.9
+// TB/s, 1.9 PFLOP/s; to fp32 280 us, 4.2 TB/s; of 6-bit rows to bf16 323 us; 128 x 2,000,000 x 768 to bf16 292 us, 4.6
+// TB/s; 256 x 32,768 x 1,024 (4 bits both) to fp32 16 us, 3.1 TB/s; 1,024 x 32,768 x 4,096 (queries do not fit LDS) to bf16
+// 270 us, 1.0 PFLOP/s.  The first keeps the matrix instructions busy for 25 % of its cycles, the vector units (exchange,
+// addresses, rounding) for 53 and LDS, from which every product reads its queries, for 40: bound by these together
+// and by the memory's latency under stores, of which two sets in flight hide a part.  Three or
 // four subtiles of rows a wave, or sets further ahead, take more registers than there are.
 #include <algorithm>
 
@@ -418,7 +419,7 @@ hipError_t launch(ScoresArgs p, hipStream_t s) {
   const long long items = (long long)p.n_qblocks * p.n_chunks;
   // All query blocks of a chunk that wait for the same tile wait for memory every time; in turned orders each tile is
   // in their L2 after the first one's wait.  As long as that holds them all: 3.5 of its 4 MB, the chunks of 32 CUs.
-  // (1,024 x 262,144 x 768, 6 and 4 bits to bf16: in one order 342 us, of 2 tiles 330, of 4 325, of 8 288, of 16 326.)
+  // (1,024 x 262,144 x 768, 6 and 4 bits to bf16: in one order 236 us, of 2 tiles 228, of 4 215, of 8 220, of 16 239.)
   const long long bytes = (long long)kRows * p.r.nb * (4 * RB + 1) * std::max(1, 32 / p.n_qblocks);
   p.turn = 1;
   while (p.turn < 8 && 2 * p.turn <= p.n_qblocks && 2 * p.turn * bytes <= 7 << 19) p.turn *= 2;
