@@ -20,7 +20,8 @@
 //
 // Measured, the step (bytes read and written once): 1,024 x 32,768 of fp32 55 us, 4.8 TB/s (a large copy: 4.76), of bf16 36 us,
 // 3.7 TB/s (two rounds of workgroups, whose conversions and exponentials memory waits for); 1,024 x 20,000 of fp32 33 us;
-// 32 x 1,000,000 of fp32 61 us, 4.2 TB/s over two reads.  The loss alone of 1,024 x 32,768 31 and 22 us.
+// 32 x 1,000,000 of fp32 61 us, 4.2 TB/s (and a second read, which the last-level cache serves).  The loss alone of
+// 1,024 x 32,768 31 and 22 us.
 #include <algorithm>
 #include <cmath>
 
