@@ -66,13 +66,13 @@ def fit(n=8192, dim=256, batch=256, k=32, steps=60, lr=0.02, seed=1):
     first, second = torch.zeros_like(weight), torch.zeros_like(weight)
     held_out = queries()
 
-    def judge():
+    def held_out_quality():
         features, ids, t = held_out
         s = student_scores(features, weight, few_bits)
         loss, _ = oprag.distill_loss(s, ids, t, temperature=TAU, teacher_temperature=TEACHER_TAU)
         return loss.mean().item(), recall(s, ids)
 
-    before = judge()
+    before = held_out_quality()
     for step in range(1, steps + 1):
         features, ids, t = queries()
         s = student_scores(features, weight, few_bits)
@@ -82,7 +82,7 @@ def fit(n=8192, dim=256, batch=256, k=32, steps=60, lr=0.02, seed=1):
         second.mul_(0.99).addcmul_(dw, dw, value=0.01)
         fix1, fix2 = 1 - 0.9 ** step, 1 - 0.99 ** step
         weight -= lr * (first / fix1) / ((second / fix2).sqrt() + 1e-8)
-    return before, judge()
+    return before, held_out_quality()
 
 
 def main():
